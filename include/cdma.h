@@ -302,6 +302,97 @@ int cdma_rle_decompress_async(const void* d_src, uint64_t src_bytes, const uint6
                               uint64_t* h_result);
 
 /* ------------------------------------------------------------------------ *
+ * Operators that make sparse maps: dropout and the gated feed-forward block of
+ * a transformer.  The method compresses what a ReLU leaves (Section IV); these
+ * are the layers whose maps have such zeros outside convolutional networks.
+ * Matrices are rows of elements with a row stride "ld" in elements (0 = dense
+ * rows); element types CDMA_F32, CDMA_F16, CDMA_BF16.  All arithmetic is in 32
+ * bits, a result is rounded to its type once.  Every pointer must be 16-byte
+ * aligned; strides and sizes are free (multiples of 16 bytes run fastest).
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Dropout with a mask that is never stored: y = residual + (kept ? x * scale : 0)
+ * for a rows x cols matrix.  With T = p * 65536 rounded to the nearest integer
+ * (halves up), scale = 65536 / (65536 - T), and element (row, col) is dropped when
+ * its 16-bit random lane is below T: lane col % 8 of the Philox4x32-10 block
+ * (Salmon, Moraes, Dror, Shaw, SC 2011) with the counter words (col / 8, row,
+ * sequence low, sequence high) and the key words (seed low, seed high); lane j is
+ * the low (j even) or high half of word j / 2.  A dropped element counts as +0
+ * whatever x holds there.  p = 0 drops nothing, p = 1 everything.
+ *
+ *   d_residual   NULL, or a matrix that is added (stride ld_residual)
+ *   rows, cols   rows < 2^32, cols <= 2^34, rows * cols <= 2^40; either may be 0
+ *   d_y          may be d_x or d_residual itself with the same stride (in place);
+ *                any other overlap is INVALID_ARG
+ *
+ * cdma_dropout_backward is dx = kept ? dy * scale : 0 for the same p, seed and
+ * sequence (the gradient of the residual is dy itself).  Both only enqueue on the
+ * stream and return a status; nothing can fail on the device, so there is no
+ * result word to wait for.
+ */
+int cdma_dropout(const void* d_x, uint64_t ld_x, const void* d_residual, uint64_t ld_residual,
+                 uint64_t rows, uint64_t cols, int dtype, double p, uint64_t seed, uint64_t sequence,
+                 void* d_y, uint64_t ld_y, void* cuda_stream);
+int cdma_dropout_backward(const void* d_dy, uint64_t ld_dy, uint64_t rows, uint64_t cols, int dtype,
+                          double p, uint64_t seed, uint64_t sequence, void* d_dx, uint64_t ld_dx,
+                          void* cuda_stream);
+
+/* Activations of the gate.  CDMA_ACT_RELU: g where g > 0 or NaN, else +0, with derivative 1 where
+ * g was kept, as the fused ReLU above; CDMA_ACT_SILU: g / (1 + e^-g); CDMA_ACT_GELU: g Phi(g), Phi
+ * the normal distribution function (not its tanh approximation). */
+enum { CDMA_ACT_RELU = 0, CDMA_ACT_SILU = 1, CDMA_ACT_GELU = 2 };
+
+/* One gated feed-forward block.  Strides of 0 stand for dense rows.  k, f <= 2^21, m < 2^31,
+ * strides <= 2^31. */
+typedef struct {
+    uint64_t m, k, f;              /* tokens, model width, hidden width */
+    uint64_t ld_x, ld_wg, ld_wu;   /* strides of x [m,k], Wg [f,k], Wu [f,k] */
+    uint64_t ld_h;                 /* of h [m,f] (forward) or dh (backward) */
+    uint64_t ld_dx, ld_dw;         /* of dx [m,k]; of dWg and dWu [f,k] */
+    int32_t dtype, activation;
+    double dropout_p;              /* dropout on h, as cdma_dropout of the m x f matrix; 0 = none */
+    uint64_t dropout_seed, dropout_sequence;
+} cdma_gated_ffn_desc;
+
+/* Bytes of device scratch of a forward (backward = 0) or backward (1) call; 0 for a
+ * descriptor that the calls refuse.  The backward pass keeps the gradients of G and U
+ * there (2 m f elements). */
+uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int backward);
+
+/*
+ * Forward: h = D act(G) U with G = x Wg^T, U = x Wu^T and D the dropout factors of
+ * h's elements (elementwise products).  G and U never reach memory.
+ *
+ * Backward: from x, Wg, Wu and dh, with e = D dh: dU = e act(G), dG = e U act'(G),
+ * dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.  G and U are computed again from the
+ * inputs: the forward pass leaves nothing to keep.  For 2-byte types dG and dU are
+ * rounded to the element type between the two products.  d_dx may be NULL, and d_dwg
+ * and d_dwu both may, when that gradient is not wanted (not all three).
+ *
+ * Outputs must not overlap inputs, one another or the workspace, except as disjoint
+ * columns of one buffer with one stride.  A size of zero is served: outputs with
+ * elements are then zero.  d_workspace as sized above, 16-byte aligned, contents
+ * irrelevant; h_result as for cdma_zvc_compress_async.  The plain forms wait for the
+ * stream and return the bytes of the outputs written or -status; the _async forms only
+ * enqueue, with h_result[0] = those bytes.
+ */
+int64_t cdma_gated_ffn_forward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg,
+                               const void* d_wu, void* d_h, void* d_workspace,
+                               uint64_t workspace_bytes, void* cuda_stream);
+int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg,
+                                 const void* d_wu, void* d_h, void* d_workspace,
+                                 uint64_t workspace_bytes, void* cuda_stream, uint64_t* h_result);
+int64_t cdma_gated_ffn_backward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg,
+                                const void* d_wu, const void* d_dh, void* d_dx, void* d_dwg,
+                                void* d_dwu, void* d_workspace, uint64_t workspace_bytes,
+                                void* cuda_stream);
+int cdma_gated_ffn_backward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg,
+                                  const void* d_wu, const void* d_dh, void* d_dx, void* d_dwg,
+                                  void* d_dwu, void* d_workspace, uint64_t workspace_bytes,
+                                  void* cuda_stream, uint64_t* h_result);
+
+/* ------------------------------------------------------------------------ *
  * Offload pipeline (Section III, Fig. 2b: OFF(n) in the forward pass, PRE(n)
  * in reverse order in the backward pass; Section V-D: the compressed copy
  * replaces the cudaMemcpy calls of the memory manager).
@@ -420,14 +511,14 @@ int64_t cdma_zvc_decompress_host(cdma_ctx* ctx, const void* h_src, uint64_t src_
                                  void* h_dst);
 
 /* Measurement hook: the next codec kernel this thread launches (compress or
- * decompress, through any entry point) is bracketed by cudaEventRecord of the
- * two given cudaEvent_t handles on the launch stream, around the kernel alone
- * (not the workspace reset or the result copy of the call).  One-shot: the pair
+ * decompress, through any entry point; for the operators the kernels of the next
+ * call) is bracketed by cudaEventRecord of the two given cudaEvent_t handles on
+ * the launch stream, around the kernel alone (not the result copy of the call).  One-shot: the pair
  * is forgotten after that launch.  Pass NULLs to cancel. */
 void cdma_time_next_kernel(void* start_event, void* stop_event);
 
 /* Number of kernel launches this library has issued in this process (codec
- * kernels and the copy kernel of cdma_offload_async; copies by the copy engines
+ * and operator kernels and the copy kernel of cdma_offload_async; copies by the copy engines
  * are not counted). */
 uint64_t cdma_kernel_launch_count(void);
 

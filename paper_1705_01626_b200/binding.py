@@ -9,7 +9,7 @@ is no CPU implementation behind these calls: if the library cannot be loaded
 from __future__ import annotations
 
 import ctypes
-from ctypes import POINTER, c_char_p, c_int, c_int64, c_uint32, c_uint64, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_int, c_int32, c_int64, c_uint32, c_uint64, c_void_p
 
 from . import _build
 
@@ -29,12 +29,22 @@ F32, F16, BF16, U8 = 0, 1, 2, 3
 NCHW, NHWC, CHWN = 0, 1, 2
 LAYOUT_CODES = {"NCHW": NCHW, "NHWC": NHWC, "CHWN": CHWN}
 
+ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2
+
 WINDOW = 32
 CHUNK = 1024
 
 
 class cdma_ticket(ctypes.Structure):
     _fields_ = [("id", c_uint64)]
+
+
+class cdma_gated_ffn_desc(ctypes.Structure):
+    """One gated feed-forward block: sizes, row strides in elements (0 = dense), types, dropout on h."""
+    _fields_ = [("m", c_uint64), ("k", c_uint64), ("f", c_uint64), ("ld_x", c_uint64), ("ld_wg", c_uint64),
+                ("ld_wu", c_uint64), ("ld_h", c_uint64), ("ld_dx", c_uint64), ("ld_dw", c_uint64),
+                ("dtype", c_int32), ("activation", c_int32), ("dropout_p", c_double),
+                ("dropout_seed", c_uint64), ("dropout_sequence", c_uint64)]
 
 
 class CdmaError(RuntimeError):
@@ -75,6 +85,19 @@ _SIGNATURES = {
                                       c_void_p, c_uint64, c_void_p]),
     "cdma_rle_decompress_async": (c_int, [c_void_p, c_uint64, c_void_p, c_uint64, c_int, c_int, c_void_p,
                                           c_void_p, c_uint64, c_void_p, c_void_p]),
+    "cdma_dropout": (c_int, [c_void_p, c_uint64, c_void_p, c_uint64, c_uint64, c_uint64, c_int, c_double, c_uint64,
+                             c_uint64, c_void_p, c_uint64, c_void_p]),
+    "cdma_dropout_backward": (c_int, [c_void_p, c_uint64, c_uint64, c_uint64, c_int, c_double, c_uint64, c_uint64,
+                                      c_void_p, c_uint64, c_void_p]),
+    "cdma_gated_ffn_workspace_bytes": (c_uint64, [POINTER(cdma_gated_ffn_desc), c_int]),
+    "cdma_gated_ffn_forward": (c_int64, [POINTER(cdma_gated_ffn_desc), c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_uint64, c_void_p]),
+    "cdma_gated_ffn_forward_async": (c_int, [POINTER(cdma_gated_ffn_desc), c_void_p, c_void_p, c_void_p, c_void_p,
+                                             c_void_p, c_uint64, c_void_p, c_void_p]),
+    "cdma_gated_ffn_backward": (c_int64, [POINTER(cdma_gated_ffn_desc), c_void_p, c_void_p, c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_void_p, c_void_p, c_uint64, c_void_p]),
+    "cdma_gated_ffn_backward_async": (c_int, [POINTER(cdma_gated_ffn_desc), c_void_p, c_void_p, c_void_p, c_void_p,
+                                              c_void_p, c_void_p, c_void_p, c_void_p, c_uint64, c_void_p, c_void_p]),
     "cdma_ctx_create": (c_int, [c_uint64, c_uint64, POINTER(c_void_p)]),
     "cdma_ctx_destroy": (c_int, [c_void_p]),
     "cdma_offload": (c_int64, [c_void_p, c_void_p, c_uint64, c_int, c_int, c_void_p, POINTER(cdma_ticket)]),
@@ -235,6 +258,51 @@ def cdma_zvc_relu_backward_async(d_src, src_bytes, d_table, n, dtype, layout, d_
     return int(lib().cdma_zvc_relu_backward_async(_vp(d_src), src_bytes, _vp(d_table), n, dtype, layout, _vp(d_dy),
                                                   _vp(d_dx), _vp(d_workspace), workspace_bytes, _vp(cuda_stream),
                                                   _vp(h_result)))
+
+
+def cdma_dropout(d_x, ld_x, d_residual, ld_residual, rows, cols, dtype, p, seed, sequence, d_y, ld_y,
+                 cuda_stream=0) -> int:
+    """y = residual + (kept ? x * scale : 0); the mask is a function of (seed, sequence, row, col).
+    d_residual may be 0.  Only enqueues; returns a status."""
+    return int(lib().cdma_dropout(_vp(d_x), ld_x, _vp(d_residual), ld_residual, rows, cols, dtype, p, seed, sequence,
+                                  _vp(d_y), ld_y, _vp(cuda_stream)))
+
+
+def cdma_dropout_backward(d_dy, ld_dy, rows, cols, dtype, p, seed, sequence, d_dx, ld_dx, cuda_stream=0) -> int:
+    """dx = kept ? dy * scale : 0 with the forward call's p, seed and sequence.  Only enqueues; returns a status."""
+    return int(lib().cdma_dropout_backward(_vp(d_dy), ld_dy, rows, cols, dtype, p, seed, sequence, _vp(d_dx), ld_dx,
+                                           _vp(cuda_stream)))
+
+
+def cdma_gated_ffn_workspace_bytes(desc, backward: int) -> int:
+    return int(lib().cdma_gated_ffn_workspace_bytes(desc, backward))
+
+
+def cdma_gated_ffn_forward(desc, d_x, d_wg, d_wu, d_h, d_workspace, workspace_bytes, cuda_stream=0) -> int:
+    """h = dropout(act(x Wg^T) * (x Wu^T)).  Returns the bytes of h, or a negative status."""
+    return int(lib().cdma_gated_ffn_forward(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_h), _vp(d_workspace),
+                                            workspace_bytes, _vp(cuda_stream)))
+
+
+def cdma_gated_ffn_forward_async(desc, d_x, d_wg, d_wu, d_h, d_workspace, workspace_bytes, cuda_stream,
+                                 h_result) -> int:
+    return int(lib().cdma_gated_ffn_forward_async(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_h), _vp(d_workspace),
+                                                  workspace_bytes, _vp(cuda_stream), _vp(h_result)))
+
+
+def cdma_gated_ffn_backward(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace, workspace_bytes,
+                            cuda_stream=0) -> int:
+    """Gradients of the block from its inputs and dh; d_dx, or d_dwg and d_dwu, may be 0.
+    Returns the bytes of the gradients written, or a negative status."""
+    return int(lib().cdma_gated_ffn_backward(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_dh), _vp(d_dx), _vp(d_dwg),
+                                             _vp(d_dwu), _vp(d_workspace), workspace_bytes, _vp(cuda_stream)))
+
+
+def cdma_gated_ffn_backward_async(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace, workspace_bytes,
+                                  cuda_stream, h_result) -> int:
+    return int(lib().cdma_gated_ffn_backward_async(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_dh), _vp(d_dx),
+                                                   _vp(d_dwg), _vp(d_dwu), _vp(d_workspace), workspace_bytes,
+                                                   _vp(cuda_stream), _vp(h_result)))
 
 
 def cdma_ctx_create(pinned_bytes: int, device_staging_bytes: int):

@@ -76,9 +76,17 @@ cudaError_t finish_result(const uint64_t* d_ws, const LaunchCtl& ctl, uint64_t* 
     return cudaMemcpyAsync(h_result, d_ws + kWsBytes, 16, cudaMemcpyDeviceToHost, stream);
 }
 
+// One thread: the result words of a call that needs no other kernel.
+static __global__ void result_kernel(uint64_t* ws, const LaunchCtl ctl, uint64_t bytes) { publish_result(ws, ctl, bytes, 0); }
+
 cudaError_t result_without_kernel(uint64_t* d_ws, uint64_t bytes, uint64_t* h_result, cudaStream_t stream) {
-    // only n = 0 comes here, where bytes is 0 too: both words are zero
-    (void)bytes;
+    if (bytes != 0) {
+        const LaunchCtl ctl = make_launch_ctl(h_result);
+        result_kernel<<<1, 1, 0, stream>>>(d_ws, ctl, bytes);
+        count_kernel_launch();
+        const cudaError_t e = cudaGetLastError();
+        return e != cudaSuccess ? e : finish_result(d_ws, ctl, h_result, stream);
+    }
     const cudaError_t e = cudaMemsetAsync(d_ws + kWsBytes, 0, 16, stream);
     if (e != cudaSuccess) return e;
     return cudaMemcpyAsync(h_result, d_ws + kWsBytes, 16, cudaMemcpyDeviceToHost, stream);

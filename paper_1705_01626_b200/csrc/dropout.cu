@@ -1,0 +1,173 @@
+// Dropout with a mask that is never stored: y = residual + (kept ? x * scale : 0), and its backward pass, which is
+// the same call on the gradient.  The mask function is in dropout.cuh, the contract in include/cdma.h.
+#include "dropout.cuh"
+#include "elements.cuh"
+#include "operand_checks.h"
+#include "zvc_common.cuh"
+
+namespace cdma {
+namespace {
+
+constexpr uint32_t kThreads = 256;
+
+// Quotient of a 32-bit number and a fixed divisor by a high product (Granlund and Montgomery, "Division by
+// invariant integers using multiplication", PLDI 1994): a tensor's blocks are numbered through its rows, and a
+// division for each would cost as much as the generator.
+struct FixedDivisor {
+    uint32_t divisor, multiplier, shift1, shift2;
+};
+FixedDivisor make_divisor(uint32_t d) {
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    FixedDivisor f;
+    f.divisor = d;
+    f.multiplier = static_cast<uint32_t>((((1ull << l) - d) << 32) / d + 1);
+    f.shift1 = l < 1 ? l : 1;
+    f.shift2 = l < 1 ? 0 : l - 1;
+    return f;
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const FixedDivisor& f) {
+    const uint32_t t = __umulhi(f.multiplier, n);
+    return (t + ((n - t) >> f.shift1)) >> f.shift2;
+}
+
+template <typename T> struct Args {
+    const T* x;
+    const T* residual;
+    T* y;
+    uint64_t ld_x, ld_r, ld_y;
+    uint64_t cols;
+    uint32_t first_row;       // of this launch
+    uint32_t blocks;          // 8-element blocks of this launch
+    FixedDivisor per_row;     // blocks per row
+    DropoutSpec drop;
+};
+
+template <typename T>
+__device__ __forceinline__ T one_element(const Args<T>& a, uint64_t ix, uint64_t ir, bool keep) {
+    const float v = keep ? to_float(a.x[ix]) * a.drop.scale : 0.0f;
+    return from_float<T>(a.residual != nullptr ? to_float(a.residual[ir]) + v : v);
+}
+
+// One thread, one block of eight elements: 16-byte loads and stores.
+template <typename T, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(const Args<T> a) {
+    constexpr int kVecs = sizeof(T) * 8 / 16;
+    const uint32_t q = blockIdx.x * kThreads + threadIdx.x;
+    if (q >= a.blocks) return;
+    const uint32_t r = divide(q, a.per_row);
+    const uint32_t block = q - r * a.per_row.divisor, row = a.first_row + r;
+    const uint64_t col = static_cast<uint64_t>(block) * 8;
+    const uint64_t ix = row * a.ld_x + col, ir = row * a.ld_r + col, iy = row * a.ld_y + col;
+    if (col + 8 > a.cols) {      // the ragged end of a row
+        const uint32_t keep = dropout_keep8(a.drop, row, block);
+        for (uint32_t j = 0; col + j < a.cols; ++j) a.y[iy + j] = one_element(a, ix + j, ir + j, (keep >> j) & 1u);
+        return;
+    }
+    uint4 xv[kVecs], rv[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        xv[i] = reinterpret_cast<const uint4*>(a.x + ix)[i];
+        if (RESIDUAL) rv[i] = reinterpret_cast<const uint4*>(a.residual + ir)[i];
+    }
+    const uint32_t keep = dropout_keep8(a.drop, row, block);
+    const T* xe = reinterpret_cast<const T*>(xv);
+    const T* re = reinterpret_cast<const T*>(rv);
+    uint4 yv[kVecs];
+    T* ye = reinterpret_cast<T*>(yv);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float v = (keep >> j) & 1u ? to_float(xe[j]) * a.drop.scale : 0.0f;
+        ye[j] = from_float<T>(RESIDUAL ? to_float(re[j]) + v : v);
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) reinterpret_cast<uint4*>(a.y + iy)[i] = yv[i];
+}
+
+// Rows that do not start on 16 bytes: a lane computes the keep bits of one block, then the warp walks its 32 blocks
+// four at a time, a lane an element, so that loads and stores stay contiguous.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) dropout_ragged_kernel(const Args<T> a) {
+    const uint32_t q = blockIdx.x * kThreads + threadIdx.x;
+    uint32_t r = 0, block = 0, keep = 0;
+    const bool there = q < a.blocks;
+    if (there) {
+        r = divide(q, a.per_row);
+        block = q - r * a.per_row.divisor;
+        keep = dropout_keep8(a.drop, a.first_row + r, block);
+    }
+    const uint32_t sub = lane_id() & 7u;
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t from = 4 * i + (lane_id() >> 3);
+        const uint32_t row = a.first_row + __shfl_sync(0xffffffffu, r, from);
+        const uint32_t b = __shfl_sync(0xffffffffu, block, from), k = __shfl_sync(0xffffffffu, keep, from);
+        const bool t = __shfl_sync(0xffffffffu, there, from);
+        const uint64_t col = static_cast<uint64_t>(b) * 8 + sub;
+        if (t && col < a.cols)
+            a.y[row * a.ld_y + col] = one_element(a, row * a.ld_x + col, row * a.ld_r + col, (k >> sub) & 1u);
+    }
+}
+
+template <typename T>
+cudaError_t launch(const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r, uint64_t rows, uint64_t cols,
+                   const DropoutSpec& drop, void* y, uint64_t ld_y, cudaStream_t stream) {
+    Args<T> a{static_cast<const T*>(x), static_cast<const T*>(residual), static_cast<T*>(y), ld_x, ld_r, ld_y, cols,
+              0, 0, make_divisor(static_cast<uint32_t>((cols + 7) / 8)), drop};
+    constexpr uint64_t kPer16 = 16 / sizeof(T);
+    const bool vectors = rows == 1 || (ld_x % kPer16 == 0 && ld_y % kPer16 == 0 && (residual == nullptr || ld_r % kPer16 == 0));
+    // a launch numbers its blocks in 32 bits, whole rows at a time
+    const uint64_t most_rows = 0x80000000ull / a.per_row.divisor > 0 ? 0x80000000ull / a.per_row.divisor : 1;
+    timing_before_launch(stream);
+    for (uint64_t row = 0; row < rows; row += most_rows) {
+        const uint64_t n = rows - row < most_rows ? rows - row : most_rows;
+        a.first_row = static_cast<uint32_t>(row);
+        a.blocks = static_cast<uint32_t>(n * a.per_row.divisor);
+        const uint32_t grid = static_cast<uint32_t>((static_cast<uint64_t>(a.blocks) + kThreads - 1) / kThreads);
+        if (!vectors) dropout_ragged_kernel<T><<<grid, kThreads, 0, stream>>>(a);
+        else if (residual != nullptr) dropout_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
+        else dropout_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
+        count_kernel_launch();
+    }
+    timing_after_launch(stream);
+    return cudaGetLastError();
+}
+
+}  // namespace
+}  // namespace cdma
+
+using namespace cdma;
+
+extern "C" {
+
+int cdma_dropout(const void* d_x, uint64_t ld_x, const void* d_residual, uint64_t ld_residual, uint64_t rows,
+                 uint64_t cols, int dtype, double p, uint64_t seed, uint64_t sequence, void* d_y, uint64_t ld_y,
+                 void* cuda_stream) {
+    if (dtype != CDMA_F32 && dtype != CDMA_F16 && dtype != CDMA_BF16) return CDMA_ERR_UNSUPPORTED_DTYPE;
+    const uint32_t s = cdma_dtype_size(dtype);
+    DropoutSpec drop;
+    if (!make_dropout_spec(p, seed, sequence, &drop)) return CDMA_ERR_INVALID_ARG;
+    if (rows > 0xffffffffull || cols > (1ull << 34) || (rows != 0 && cols > (1ull << 40) / rows)) return CDMA_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return CDMA_OK;
+    Operand x, r, y;
+    if (!make_operand(d_x, rows, cols, ld_x, s, &x) || !make_operand(d_y, rows, cols, ld_y, s, &y)) return CDMA_ERR_INVALID_ARG;
+    if (d_residual != nullptr && !make_operand(d_residual, rows, cols, ld_residual, s, &r)) return CDMA_ERR_INVALID_ARG;
+    if (!starts_on_16(d_x) || !starts_on_16(d_y) || !starts_on_16(d_residual)) return CDMA_ERR_ALIGNMENT;
+    // in place (the same elements at the same place) is fine, any other overlap is not
+    if (!same_place(x, y) && overlap(x, y)) return CDMA_ERR_INVALID_ARG;
+    if (d_residual != nullptr && !same_place(r, y) && overlap(r, y)) return CDMA_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = cudaSuccess;
+    const uint64_t ld_r = d_residual != nullptr ? r.ld : 0;
+    if (dtype == CDMA_F32) e = launch<float>(d_x, x.ld, d_residual, ld_r, rows, cols, drop, d_y, y.ld, stream);
+    else if (dtype == CDMA_F16) e = launch<__half>(d_x, x.ld, d_residual, ld_r, rows, cols, drop, d_y, y.ld, stream);
+    else e = launch<__nv_bfloat16>(d_x, x.ld, d_residual, ld_r, rows, cols, drop, d_y, y.ld, stream);
+    return e == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+}
+
+int cdma_dropout_backward(const void* d_dy, uint64_t ld_dy, uint64_t rows, uint64_t cols, int dtype, double p,
+                          uint64_t seed, uint64_t sequence, void* d_dx, uint64_t ld_dx, void* cuda_stream) {
+    return cdma_dropout(d_dy, ld_dy, nullptr, 0, rows, cols, dtype, p, seed, sequence, d_dx, ld_dx, cuda_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,162 @@
+// extern "C" entry points of the gated feed-forward block: argument checking, dispatch, result hand-over.
+// Declarations and contracts are in include/cdma.h.
+#include "gated_ffn.cuh"
+#include "operand_checks.h"
+
+namespace cdma {
+namespace {
+
+constexpr uint64_t kMaxRows = (1ull << 31) - 1;
+constexpr uint64_t kMaxWidth = 1ull << 21;      // of k and f
+
+int check_desc(const cdma_gated_ffn_desc* d, DropoutSpec* drop) {
+    if (d == nullptr) return CDMA_ERR_INVALID_ARG;
+    if (d->dtype != CDMA_F32 && d->dtype != CDMA_F16 && d->dtype != CDMA_BF16) return CDMA_ERR_UNSUPPORTED_DTYPE;
+    if (d->activation != CDMA_ACT_RELU && d->activation != CDMA_ACT_SILU && d->activation != CDMA_ACT_GELU)
+        return CDMA_ERR_INVALID_ARG;
+    if (d->m > kMaxRows || d->k > kMaxWidth || d->f > kMaxWidth) return CDMA_ERR_INVALID_ARG;
+    if (!make_dropout_spec(d->dropout_p, d->dropout_seed, d->dropout_sequence, drop)) return CDMA_ERR_INVALID_ARG;
+    const uint64_t ld[6] = {d->ld_x, d->ld_wg, d->ld_wu, d->ld_dx, d->ld_dw, d->ld_h};
+    for (int i = 0; i < 6; ++i)
+        if (ld[i] != 0 && (ld[i] < (i < 5 ? d->k : d->f) || ld[i] > (1ull << 31))) return CDMA_ERR_INVALID_ARG;
+    return CDMA_OK;
+}
+
+uint64_t or_dense(uint64_t ld, uint64_t cols) { return ld != 0 ? ld : cols; }
+
+uint64_t workspace_of(const cdma_gated_ffn_desc& d, bool backward) {
+    const uint64_t bytes = kFfnWsHeader + ffn_simt_workspace(d.m, d.f, cdma_dtype_size(d.dtype), backward);
+    return (bytes + 255) & ~255ull;
+}
+
+// Checks shared by the two passes: dh and the gradients are null in the forward pass, h in the backward pass.
+int make_problem(const cdma_gated_ffn_desc* d, bool backward, const void* x, const void* wg, const void* wu, void* h,
+                 const void* dh, void* dx, void* dwg, void* dwu, void* ws, uint64_t ws_bytes, uint64_t* h_result,
+                 FfnProblem* p) {
+    DropoutSpec drop;
+    const int st = check_desc(d, &drop);
+    if (st != CDMA_OK) return st;
+    if (h_result == nullptr || ws == nullptr) return CDMA_ERR_INVALID_ARG;
+    // (a matrix without elements may well have no address)
+    if (backward && d->k != 0 && d->f != 0 && (dwg == nullptr) != (dwu == nullptr)) return CDMA_ERR_INVALID_ARG;
+    if (backward && d->k != 0 && (d->m != 0 || d->f != 0) && dx == nullptr && dwg == nullptr) return CDMA_ERR_INVALID_ARG;
+    const uint64_t s = cdma_dtype_size(d->dtype);
+    // the matrices of the call: three or four inputs, then the outputs
+    Operand in[4], out[3];
+    int n_in = 0, n_out = 0;
+    bool fine = make_operand(x, d->m, d->k, d->ld_x, s, &in[n_in++]);
+    fine = make_operand(wg, d->f, d->k, d->ld_wg, s, &in[n_in++]) && fine;
+    fine = make_operand(wu, d->f, d->k, d->ld_wu, s, &in[n_in++]) && fine;
+    if (backward) {
+        fine = make_operand(dh, d->m, d->f, d->ld_h, s, &in[n_in++]) && fine;
+        if (dx != nullptr) fine = make_operand(dx, d->m, d->k, d->ld_dx, s, &out[n_out++]) && fine;
+        if (dwg != nullptr && dwu != nullptr) {
+            fine = make_operand(dwg, d->f, d->k, d->ld_dw, s, &out[n_out++]) && fine;
+            fine = make_operand(dwu, d->f, d->k, d->ld_dw, s, &out[n_out++]) && fine;
+        }
+    } else {
+        fine = make_operand(h, d->m, d->f, d->ld_h, s, &out[n_out++]) && fine;
+    }
+    if (!fine) return CDMA_ERR_INVALID_ARG;
+    const void* all[] = {x, wg, wu, h, dh, dx, dwg, dwu, ws};
+    for (const void* q : all)
+        if (!starts_on_16(q)) return CDMA_ERR_ALIGNMENT;
+    if (ws_bytes < workspace_of(*d, backward)) return CDMA_ERR_BUFFER_TOO_SMALL;
+    Operand w;
+    make_operand(ws, 1, ws_bytes, 0, 1, &w);
+    for (int i = 0; i < n_out; ++i) {
+        if (overlap(out[i], w)) return CDMA_ERR_INVALID_ARG;
+        for (int j = 0; j < n_in; ++j)
+            if (overlap(out[i], in[j])) return CDMA_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return CDMA_ERR_INVALID_ARG;
+    }
+    for (int j = 0; j < n_in; ++j)
+        if (overlap(in[j], w)) return CDMA_ERR_INVALID_ARG;
+    *p = FfnProblem{x, wg, wu, dh, h, dx, dwg, dwu,
+                    or_dense(d->ld_x, d->k), or_dense(d->ld_wg, d->k), or_dense(d->ld_wu, d->k), or_dense(d->ld_h, d->f),
+                    or_dense(d->ld_dx, d->k), or_dense(d->ld_dw, d->k),
+                    static_cast<uint32_t>(d->m), static_cast<uint32_t>(d->k), static_cast<uint32_t>(d->f),
+                    d->dtype, d->activation, drop, static_cast<uint64_t*>(ws),
+                    backward ? s * ((dx != nullptr ? d->m * d->k : 0) + (dwg != nullptr ? 2 * d->f * d->k : 0)) : s * d->m * d->f};
+    return CDMA_OK;
+}
+
+cudaError_t zero_rows(void* p, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t s, cudaStream_t stream) {
+    if (p == nullptr || rows == 0 || cols == 0) return cudaSuccess;
+    return cudaMemset2DAsync(p, ld * s, 0, cols * s, rows, stream);
+}
+
+// A size of zero: every sum is empty and every output, if it has elements, is zero.
+int without_kernels(const FfnProblem& p, uint64_t* h_result, cudaStream_t stream) {
+    const uint64_t s = cdma_dtype_size(p.dtype);
+    if (zero_rows(p.h, p.m, p.f, p.ld_h, s, stream) != cudaSuccess || zero_rows(p.dx, p.m, p.k, p.ld_dx, s, stream) != cudaSuccess ||
+        zero_rows(p.dwg, p.f, p.k, p.ld_dw, s, stream) != cudaSuccess || zero_rows(p.dwu, p.f, p.k, p.ld_dw, s, stream) != cudaSuccess)
+        return CDMA_ERR_CUDA;
+    return result_without_kernel(p.ws, p.result_bytes, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+}
+
+int64_t wait_for(int st, void* cuda_stream, const uint64_t* result) {
+    if (st != CDMA_OK) return -static_cast<int64_t>(st);
+    if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return -static_cast<int64_t>(CDMA_ERR_CUDA);
+    if (result[1] != 0) return -static_cast<int64_t>(result[1]);
+    return static_cast<int64_t>(result[0]);
+}
+
+}  // namespace
+}  // namespace cdma
+
+using namespace cdma;
+
+extern "C" {
+
+uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int backward) {
+    DropoutSpec drop;
+    return check_desc(desc, &drop) == CDMA_OK ? workspace_of(*desc, backward != 0) : 0;
+}
+
+int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
+                                 void* d_h, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream,
+                                 uint64_t* h_result) {
+    FfnProblem p;
+    const int st = make_problem(desc, false, d_x, d_wg, d_wu, d_h, nullptr, nullptr, nullptr, nullptr, d_workspace,
+                                workspace_bytes, h_result, &p);
+    if (st != CDMA_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
+    const LaunchCtl ctl = make_launch_ctl(h_result);
+    if (launch_ffn_simt_forward(p, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
+    return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+}
+
+int64_t cdma_gated_ffn_forward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
+                               void* d_h, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream) {
+    uint64_t result[2] = {0, 0};
+    const int st = cdma_gated_ffn_forward_async(desc, d_x, d_wg, d_wu, d_h, d_workspace, workspace_bytes, cuda_stream, result);
+    return wait_for(st, cuda_stream, result);
+}
+
+int cdma_gated_ffn_backward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
+                                  const void* d_dh, void* d_dx, void* d_dwg, void* d_dwu, void* d_workspace,
+                                  uint64_t workspace_bytes, void* cuda_stream, uint64_t* h_result) {
+    FfnProblem p;
+    const int st = make_problem(desc, true, d_x, d_wg, d_wu, nullptr, d_dh, d_dx, d_dwg, d_dwu, d_workspace,
+                                workspace_bytes, h_result, &p);
+    if (st != CDMA_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
+    const LaunchCtl ctl = make_launch_ctl(h_result);
+    if (launch_ffn_simt_backward(p, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
+    return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+}
+
+int64_t cdma_gated_ffn_backward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
+                                const void* d_dh, void* d_dx, void* d_dwg, void* d_dwu, void* d_workspace,
+                                uint64_t workspace_bytes, void* cuda_stream) {
+    uint64_t result[2] = {0, 0};
+    const int st = cdma_gated_ffn_backward_async(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace,
+                                                 workspace_bytes, cuda_stream, result);
+    return wait_for(st, cuda_stream, result);
+}
+
+}  // extern "C"

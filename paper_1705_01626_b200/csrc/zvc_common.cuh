@@ -172,7 +172,7 @@ LaunchCtl make_launch_ctl(uint64_t* h_result);                  // fresh tag; re
 bool in_host_memory(const void* p);                              // p lies in page-locked host memory
 // After the kernel: hand the result words to h_result unless the kernel stores them there itself.
 cudaError_t finish_result(const uint64_t* d_ws, const LaunchCtl& ctl, uint64_t* h_result, cudaStream_t stream);
-// A call that launches no kernel (n = 0): result words {bytes, 0} by plain stream operations.
+// A call without a kernel of its own (a size of zero): result words {bytes, 0}.
 cudaError_t result_without_kernel(uint64_t* d_ws, uint64_t bytes, uint64_t* h_result, cudaStream_t stream);
 // cudaFuncSetAttribute(MaxDynamicSharedMemorySize) once per kernel and device instead of on every launch.
 cudaError_t opt_in_shared_memory(const void* kernel, uint32_t bytes);

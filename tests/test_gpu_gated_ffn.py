@@ -1,0 +1,279 @@
+"""GPU: cdma_gated_ffn_forward / _backward against the formulas in 64 bits, element by element within the bounds that
+oracle/gated_ffn.py derives; the padding of every strided output and the bytes behind the workspace stay untouched."""
+import math
+
+import pytest
+import torch
+
+from oracle import dropout_numpy as dn
+from oracle import gated_ffn as gf
+from paper_1705_01626_b200 import binding as B
+from tests.gpu_helpers import CANARY, DT
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.float32, torch.float16, torch.bfloat16]
+ACTS = {"relu": B.ACT_RELU, "silu": B.ACT_SILU, "gelu": B.ACT_GELU}
+
+
+class Block:
+    """Inputs and outputs of one call; pads: extra columns of x, Wg, Wu, h/dh, dx, dWg/dWu."""
+
+    def __init__(self, m, k, f, dtype, act="silu", p=0.0, seed=5, sequence=6, pads=(0, 0, 0, 0, 0, 0), rng=1):
+        self.m, self.k, self.f, self.dtype, self.act, self.p, self.seed, self.sequence = m, k, f, dtype, act, p, seed, sequence
+        g = torch.Generator(device="cuda").manual_seed(rng + 7 * m + 11 * k + 13 * f)
+
+        def wide(rows, cols, pad, scale=None):
+            t = torch.full((rows, cols + pad), 7.0, dtype=dtype, device="cuda")
+            if scale is not None:
+                t[:, :cols] = (torch.randn(rows, cols, generator=g, device="cuda") * scale).to(dtype)
+            return t
+
+        self.xw, self.wgw, self.wuw = wide(m, k, pads[0], 1.0), wide(f, k, pads[1], max(k, 1) ** -0.5), wide(f, k, pads[2], max(k, 1) ** -0.5)
+        self.dhw = wide(m, f, pads[3], 0.1)
+        self.hw, self.dxw = wide(m, f, pads[3]), wide(m, k, pads[4])
+        self.dwgw, self.dwuw = wide(f, k, pads[5]), wide(f, k, pads[5])
+        self.x, self.wg, self.wu, self.dh = self.xw[:, :k], self.wgw[:, :k], self.wuw[:, :k], self.dhw[:, :f]
+        self.desc = B.cdma_gated_ffn_desc(
+            m=m, k=k, f=f, ld_x=k + pads[0], ld_wg=k + pads[1], ld_wu=k + pads[2], ld_h=f + pads[3], ld_dx=k + pads[4],
+            ld_dw=k + pads[5], dtype=DT[dtype], activation=ACTS[act], dropout_p=p, dropout_seed=seed, dropout_sequence=sequence)
+
+    def workspace(self, backward):
+        self.ws_bytes = B.cdma_gated_ffn_workspace_bytes(self.desc, backward)
+        self.ws = torch.full((self.ws_bytes + 256,), CANARY, dtype=torch.uint8, device="cuda")
+
+    def forward(self, stream=0):
+        self.workspace(0)
+        r = B.cdma_gated_ffn_forward(self.desc, self.x.data_ptr(), self.wg.data_ptr(), self.wu.data_ptr(), self.hw.data_ptr(),
+                                     self.ws.data_ptr(), self.ws_bytes, stream)
+        assert r == self.m * self.f * self.x.element_size(), B.status_string(r)
+        assert (self.ws[self.ws_bytes:] == CANARY).all() and (self.hw[:, self.f:] == 7.0).all()
+        return self.hw[:, :self.f]
+
+    def backward(self, stream=0, dx=True, dw=True):
+        self.workspace(1)
+        r = B.cdma_gated_ffn_backward(self.desc, self.x.data_ptr(), self.wg.data_ptr(), self.wu.data_ptr(), self.dh.data_ptr(),
+                                      self.dxw.data_ptr() if dx else 0, self.dwgw.data_ptr() if dw else 0,
+                                      self.dwuw.data_ptr() if dw else 0, self.ws.data_ptr(), self.ws_bytes, stream)
+        assert r == self.x.element_size() * ((self.m * self.k if dx else 0) + (2 * self.f * self.k if dw else 0)), B.status_string(r)
+        assert (self.ws[self.ws_bytes:] == CANARY).all()
+        for t in (self.dxw, self.dwgw, self.dwuw):
+            assert (t[:, self.k:] == 7.0).all()
+        return {"dx": self.dxw[:, :self.k], "dwg": self.dwgw[:, :self.k], "dwu": self.dwuw[:, :self.k]}
+
+    def check_forward(self, stream=0):
+        h = self.forward(stream)
+        want = gf.forward(self.x, self.wg, self.wu, self.act, self.p, self.seed, self.sequence)
+        within(h, want, "h")
+        return h
+
+    def check_backward(self, stream=0):
+        got = self.backward(stream)
+        want = gf.backward(self.x, self.wg, self.wu, self.dh, self.act, self.p, self.seed, self.sequence)
+        for n in got:
+            within(got[n], want, n)
+        return got
+
+
+def within(got, want, name):
+    off = (got.double() - want.value[name]).abs()
+    worst = (off / want.bound[name].clamp(min=1e-300)).max() if off.numel() else 0
+    assert torch.isfinite(got).all() and worst <= 1, "%s: %.3g of its bound" % (name, float(worst))
+
+
+SIZES = [(1, 1, 1), (1, 64, 128), (1, 1000, 77), (2, 33, 5), (3, 64, 256), (7, 200, 130), (16, 512, 256), (17, 1024, 136),
+         (31, 72, 1000), (33, 128, 64), (64, 256, 512), (65, 136, 129), (127, 65, 127), (128, 64, 128), (129, 130, 131),
+         (200, 512, 384), (255, 257, 259), (256, 128, 256), (257, 192, 520), (300, 1001, 311), (513, 320, 640)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,f", SIZES)
+def test_matches_the_formulas(m, k, f, dtype):
+    act = ("relu", "silu", "gelu")[(m + k + f) % 3]
+    p = (0.0, 0.25)[(m + f) % 2]
+    b = Block(m, k, f, dtype, act, p)
+    b.check_forward()
+    b.check_backward()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("m", [1, 5, 40, 300])
+def test_activations_and_dropout(act, dtype, m):
+    for p in (0.0, 0.5):
+        b = Block(m, 128, 264, dtype, act, p, seed=(1 << 60) + m, sequence=(7 << 35) + 1)
+        b.check_forward()
+        b.check_backward()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 20, 150])
+@pytest.mark.parametrize("pads", [(8, 16, 24, 32, 40, 48), (1, 2, 3, 4, 5, 6), (4, 4, 4, 4, 4, 4), (0, 3, 0, 1, 0, 0)])
+def test_strides(dtype, m, pads):
+    for k, f in ((128, 256), (67, 141)):
+        b = Block(m, k, f, dtype, "gelu", 0.1, pads=pads)
+        b.check_forward()
+        b.check_backward()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_both_projections_in_one_weight_buffer(dtype):
+    # gate and up projections as the halves of one [f, 2k] buffer, by rows of it, and their gradients likewise
+    m, k, f = 70, 64, 96
+    b = Block(m, k, f, dtype, "silu")
+    both = torch.cat((b.wg, b.wu), dim=1).contiguous()
+    grads = torch.zeros_like(both)
+    desc = B.cdma_gated_ffn_desc(m=m, k=k, f=f, ld_wg=2 * k, ld_wu=2 * k, ld_dw=2 * k, dtype=DT[dtype], activation=B.ACT_SILU)
+    ws = torch.empty(B.cdma_gated_ffn_workspace_bytes(desc, 1), dtype=torch.uint8, device="cuda")
+    r = B.cdma_gated_ffn_backward(desc, b.x.data_ptr(), both.data_ptr(), both[:, k:].data_ptr(), b.dh.data_ptr(), b.dxw.data_ptr(),
+                                  grads.data_ptr(), grads[:, k:].data_ptr(), ws.data_ptr(), ws.numel(), 0)
+    assert r > 0, B.status_string(r)
+    want = gf.backward(b.x, b.wg, b.wu, b.dh, "silu")
+    for got, n in ((b.dxw, "dx"), (grads[:, :k], "dwg"), (grads[:, k:], "dwu")):
+        within(got, want, n)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [3, 90])
+def test_dropout_is_that_of_the_dropout_call(dtype, m):
+    k, f, p = 96, 203, 0.4
+    plain, dropped = Block(m, k, f, dtype, "relu"), Block(m, k, f, dtype, "relu", p)
+    h = plain.forward()
+    y = torch.empty_like(h, memory_format=torch.contiguous_format)
+    assert B.cdma_dropout(h.data_ptr(), h.stride(0), 0, 0, m, f, DT[dtype], p, 5, 6, y.data_ptr(), f, 0) == B.OK
+    got = dropped.forward()
+    assert torch.equal(got == 0, y == 0)
+    # h rounded before and after the factor instead of after it alone
+    assert ((got.double() - y.double()).abs() <= 3 * gf.UNIT[dtype] * y.double().abs() + 2 * gf.TINY[dtype]).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [2, 140])
+def test_parts_of_the_gradient(dtype, m):
+    b = Block(m, 80, 120, dtype)
+    both = {n: t.clone() for n, t in b.backward().items()}
+    b.dxw.fill_(7.0)
+    b.dwgw.fill_(7.0)
+    b.dwuw.fill_(7.0)
+    assert torch.equal(b.backward(dw=False)["dx"], both["dx"]) and (b.dwgw == 7.0).all() and (b.dwuw == 7.0).all()
+    b.dxw.fill_(7.0)
+    got = b.backward(dx=False)
+    assert torch.equal(got["dwg"], both["dwg"]) and torch.equal(got["dwu"], both["dwu"]) and (b.dxw == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_sizes_of_zero(dtype):
+    for m, k, f in ((0, 8, 16), (4, 0, 16), (4, 8, 0), (0, 0, 0)):
+        b = Block(m, k, f, dtype)
+        assert (b.forward() == 0).all()
+        for t in b.backward().values():
+            assert (t == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [4, 300])
+def test_same_bits_every_time_and_on_another_stream(dtype, m):
+    b = Block(m, 300, 500, dtype, "gelu", 0.1)
+    h, grads = b.forward().clone(), {n: t.clone() for n, t in b.backward().items()}
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    assert torch.equal(b.forward(stream.cuda_stream), h)
+    got = b.backward(stream.cuda_stream)
+    assert all(torch.equal(got[n], grads[n]) for n in grads)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [6, 200])
+def test_what_is_not_finite_stays_in_its_row(dtype, m):
+    b = Block(m, 64, 96, dtype, "relu")
+    clean = b.forward().clone()
+    b.x[3, 5] = float("inf")
+    b.x[4, 0] = float("nan")
+    h = b.forward()
+    rest = [r for r in range(m) if r not in (3, 4)]
+    assert torch.equal(h[rest], clean[rest])
+    assert torch.isnan(h[4]).all()          # a ReLU keeps NaNs
+    assert not torch.isfinite(h[3]).all()
+
+
+@pytest.mark.parametrize("m", [3, 130])
+def test_dropped_places_are_zero_where_the_product_is_not_finite(m):
+    b = Block(m, 64, 96, torch.bfloat16, "silu", 0.5)
+    b.x[1] = float("nan")
+    keep = torch.from_numpy(dn.keep_mask(m, 96, 0.5, 5, 6)).cuda()
+    h = b.forward()
+    assert torch.equal(torch.isnan(h[1]), keep[1]) and (h[1][~keep[1]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [8, 130])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_saturated_gates(dtype, m, act):
+    # gates far out on both sides: e^-g overflows or vanishes, the outputs must not
+    k, f = 32, 64
+    b = Block(m, k, f, dtype, act)
+    b.x.zero_(), b.wg.zero_()
+    b.x[:, 0], b.x[:, 1] = 30.0, 1.0
+    b.wg[: f // 2, 0], b.wg[f // 2:, 0] = 4.0, -4.0       # G = 120 and -120
+    b.check_forward()
+    b.check_backward()
+
+
+def test_gradient_against_differences_of_the_forward_pass():
+    # both passes in 32 bits; L = sum(h dh) along random directions, steps of 2^-6 and 2^-7 combined so that the
+    # third-order term cancels; what is left is fifth-order and the rounding of h, each h off by its bound
+    m, k, f = 12, 40, 56
+    b = Block(m, k, f, torch.float32, "silu", 0.2)
+    grads = b.check_backward()
+    bound = float((gf.forward(b.x, b.wg, b.wu, "silu", 0.2, 5, 6).bound["h"] * b.dh.double().abs()).sum())
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for name, t in (("dx", b.x), ("dwg", b.wg), ("dwu", b.wu)):
+        v = torch.randn(t.shape, generator=g, device="cuda")
+        v /= v.norm()
+        keep = t.clone()
+
+        def loss(step):
+            t.copy_((keep.double() + step * v.double()).float())
+            value = float((b.forward().double() * b.dh.double()).sum())
+            moved = t.double() - keep.double()
+            t.copy_(keep)
+            return value, moved
+
+        def slope(step):
+            (up, a), (down, c) = loss(step), loss(-step)
+            return (up - down) / (2 * step), (a - c) / (2 * step)
+
+        (fine, vf), (coarse, vc) = slope(2.0 ** -7), slope(2.0 ** -6)
+        diff = (4 * fine - coarse) / 3
+        direction = (4 * vf - vc) / 3        # the step that the rounded inputs really took
+        want = float((grads[name].double() * direction).sum())
+        rounding = (4 * bound * 2.0 ** 7 + bound * 2.0 ** 6) / 3
+        size = float((b.dh.double().abs().sum()))
+        assert abs(diff - want) <= rounding + 2.0 ** -24 * size, (name, diff, want, rounding)
+
+
+def test_result_words_of_the_async_forms():
+    b = Block(50, 64, 96, torch.bfloat16)
+    for pinned in (True, False):
+        words = torch.full((2,), -1, dtype=torch.int64)
+        words = words.pin_memory() if pinned else words
+        b.workspace(1)
+        st = B.cdma_gated_ffn_forward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.hw.data_ptr(),
+                                            b.ws.data_ptr(), b.ws_bytes, 0, words.data_ptr())
+        torch.cuda.synchronize()
+        assert st == B.OK and words.tolist() == [50 * 96 * 2, 0]
+        st = B.cdma_gated_ffn_backward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.dh.data_ptr(),
+                                             b.dxw.data_ptr(), b.dwgw.data_ptr(), b.dwuw.data_ptr(), b.ws.data_ptr(),
+                                             b.ws_bytes, 0, words.data_ptr())
+        torch.cuda.synchronize()
+        assert st == B.OK and words.tolist() == [2 * (50 * 64 + 2 * 96 * 64), 0]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_error_as_a_whole_at_ordinary_sizes(dtype):
+    # the 2-norm of the error: one rounding of h, two of the gradients, each below 2^-p of a value
+    b = Block(600, 1024, 1408, dtype, "silu")
+    rel = lambda got, want: float((got.double() - want).norm() / want.norm())
+    assert rel(b.forward(), gf.forward(b.x, b.wg, b.wu, "silu").value["h"]) < gf.UNIT[dtype] + 2.0 ** -18
+    got, want = b.backward(), gf.backward(b.x, b.wg, b.wu, b.dh, "silu").value
+    for n in got:
+        assert rel(got[n], want[n]) < math.sqrt(2) * gf.UNIT[dtype] + 2.0 ** -18
