@@ -29,48 +29,55 @@ struct FfnProblem {
 
 constexpr uint64_t kFfnWsHeader = 256;   // bytes in front of the rest of the workspace
 
-// act(g), and with SLOPE its derivative.  A ReLU keeps NaNs and lets a gradient through where it kept its input, as
-// the fused ReLU of the codec does.
-template <int ACT>
+// act(g) and its slope.  A ReLU keeps NaNs and lets a gradient through where it kept its input, as the fused ReLU of
+// the codec does.  FAST, for results of 2-byte types: the exponential and the quotient by the hardware's
+// approximations, a few units of 2^-22 off, where the result is rounded at 2^-9 or 2^-12.
+template <bool FAST>
+__device__ __forceinline__ float logistic(float g) {
+    return FAST ? __fdividef(1.0f, 1.0f + __expf(-g)) : 1.0f / (1.0f + expf(-g));
+}
+template <int ACT, bool FAST>
 __device__ __forceinline__ float activate(float g) {
     if (ACT == CDMA_ACT_RELU) return g > 0.0f || g != g ? g : 0.0f;
-    if (ACT == CDMA_ACT_SILU) return g / (1.0f + expf(-g));
+    if (ACT == CDMA_ACT_SILU) return g * logistic<FAST>(g);
     return g * normcdff(g);
 }
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ void activate_slope(float g, float* a, float* slope) {
     if (ACT == CDMA_ACT_RELU) {
         const bool on = g > 0.0f || g != g;
         *a = on ? g : 0.0f;
         *slope = on ? 1.0f : 0.0f;
     } else if (ACT == CDMA_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
+        const float s = logistic<FAST>(g);
         *a = g * s;
         *slope = s * (1.0f + g * (1.0f - s));
     } else {
         const float cdf = normcdff(g);
         *a = g * cdf;
-        *slope = cdf + g * (0.3989422804014327f * expf(-0.5f * g * g));
+        *slope = cdf + g * (0.3989422804014327f * (FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g)));
     }
 }
 
 // Elementwise ends of the two passes; `keep` is the dropout bit of the element.
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ float gated_value(float g, float u, bool keep, float scale) {
-    return keep ? activate<ACT>(g) * u * scale : 0.0f;
+    return keep ? activate<ACT, FAST>(g) * u * scale : 0.0f;
 }
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ void gated_gradients(float g, float u, float dh, bool keep, float scale, float* dg, float* du) {
     float a, slope;
-    activate_slope<ACT>(g, &a, &slope);
+    activate_slope<ACT, FAST>(g, &a, &slope);
     const float e = dh * scale;
     *du = keep ? e * a : 0.0f;
     *dg = keep ? e * u * slope : 0.0f;
 }
 
-// Simple kernels (gated_ffn_simt.cu): any type, stride and size.
-uint64_t ffn_simt_workspace(uint64_t m, uint64_t f, uint32_t elem_size, bool backward);
-cudaError_t launch_ffn_simt_forward(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
-cudaError_t launch_ffn_simt_backward(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
+// 4-byte elements, on the ordinary arithmetic units (gated_ffn_simt.cu).
+uint64_t ffn_simt_workspace(uint64_t m, uint64_t f, bool backward);
+cudaError_t launch_ffn_simt(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream);
+// 2-byte elements, on the matrix units (gated_ffn_mma.cu).
+uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, bool backward);
+cudaError_t launch_ffn_mma(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream);
 
 }  // namespace cdma

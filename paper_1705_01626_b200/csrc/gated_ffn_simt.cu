@@ -1,5 +1,5 @@
-// The gated feed-forward block on the ordinary arithmetic units, for any type, stride and size: tiled products
-// with 128 x 128 outputs per block, 8 x 8 per thread, a reduction step of 16 staged through shared memory while the
+// The gated feed-forward block for 4-byte elements, on the ordinary arithmetic units (the matrix units would round the
+// operands to 10 or fewer bits), for any stride and size: tiled products with 128 x 128 outputs per block, 8 x 8 per thread, a reduction step of 16 staged through shared memory while the
 // next one is on its way into registers.
 #include "gated_ffn.cuh"
 
@@ -16,23 +16,15 @@ __device__ __forceinline__ void group_of(uint32_t g, uint32_t* line, uint32_t* r
     else       { *line = (g & 31) * 4; *red = g >> 5; }
 }
 
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, int64_t there, bool vectors, float v[4]) {
-    // `there` elements exist from p on
+// Four neighbours from p on, of which `there` exist.
+__device__ __forceinline__ void load4(const float* p, int64_t there, bool vectors, float v[4]) {
     if (vectors && there >= 4) {
-        if (sizeof(T) == 4) {
-            const float4 q = *reinterpret_cast<const float4*>(p);
-            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-        } else {
-            const uint2 q = *reinterpret_cast<const uint2*>(p);
-            const float2 a = unpack2<typename std::conditional<sizeof(T) == 4, __half, T>::type>(q.x);
-            const float2 b = unpack2<typename std::conditional<sizeof(T) == 4, __half, T>::type>(q.y);
-            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-        }
+        const float4 q = *reinterpret_cast<const float4*>(p);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < there ? to_float(p[i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) v[i] = i < there ? p[i] : 0.0f;
 }
 
 template <bool ALONG>
@@ -107,13 +99,13 @@ struct GateArgs {
     uint32_t x_vectors, wg_vectors, wu_vectors;
 };
 
-template <typename T, int ACT, bool BACKWARD>
+template <int ACT, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads, 2) ffn_simt_gate_kernel(const GateArgs a, const LaunchCtl ctl) {
     __shared__ __align__(16) Shared sh;
     const FfnProblem& p = a.p;
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) init_decode_result(p.ws, ctl, p.result_bytes);
     const uint32_t m0 = blockIdx.x * kTile, f0 = blockIdx.y * 64;
-    const T* x = static_cast<const T*>(p.x);
+    const float* x = static_cast<const float*>(p.x);
     float acc[8][8];
     product<true, true>(
         sh, acc, (p.k + kStep - 1) / kStep,
@@ -130,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_gate_kernel(const GateAr
             const uint32_t row = f0 + (line & 63u);
             const int64_t c = static_cast<int64_t>(step) * kStep + red;
             const bool gate = line < 64;
-            const T* w = static_cast<const T*>(gate ? p.wg : p.wu) + row * (gate ? p.ld_wg : p.ld_wu) + c;
+            const float* w = static_cast<const float*>(gate ? p.wg : p.wu) + row * (gate ? p.ld_wg : p.ld_wu) + c;
             load4(w, row < p.f ? p.k - c : 0, gate ? a.wg_vectors : a.wu_vectors, v);
         });
     const uint32_t col = f0 + (threadIdx.x & 15u) * 4;
@@ -145,12 +137,12 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_gate_kernel(const GateAr
             if (col + j >= p.f) break;
             const float g = acc[i][j], u = acc[i][j + 4];
             if (!BACKWARD) {
-                static_cast<T*>(p.h)[at + j] = from_float<T>(gated_value<ACT>(g, u, (keep >> j) & 1u, p.drop.scale));
+                static_cast<float*>(p.h)[at + j] = gated_value<ACT, false>(g, u, (keep >> j) & 1u, p.drop.scale);
             } else {
                 float dg, du;
-                gated_gradients<ACT>(g, u, to_float(static_cast<const T*>(p.dh)[at + j]), (keep >> j) & 1u, p.drop.scale, &dg, &du);
-                static_cast<T*>(a.grads)[to + j] = from_float<T>(dg);
-                static_cast<T*>(a.grads)[p.m * a.ld_grad + to + j] = from_float<T>(du);
+                gated_gradients<ACT, false>(g, u, static_cast<const float*>(p.dh)[at + j], (keep >> j) & 1u, p.drop.scale, &dg, &du);
+                static_cast<float*>(a.grads)[to + j] = dg;
+                static_cast<float*>(a.grads)[p.m * a.ld_grad + to + j] = du;
             }
         }
     }
@@ -158,13 +150,12 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_gate_kernel(const GateAr
 
 // ---- dx = [dG dU] [Wg; Wu] --------------------------------------------------------------------------------------
 
-template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) ffn_simt_dx_kernel(const GateArgs a) {
     __shared__ __align__(16) Shared sh;
     const FfnProblem& p = a.p;
     const uint32_t m0 = blockIdx.x * kTile, c0 = blockIdx.y * kTile;
     const uint32_t half = (p.f + kStep - 1) / kStep;
-    const T* grads = static_cast<const T*>(a.grads);
+    const float* grads = static_cast<const float*>(a.grads);
     float acc[8][8];
     product<true, false>(
         sh, acc, 2 * half,
@@ -182,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_dx_kernel(const GateArgs
             const bool up = step >= half;
             const uint64_t row = static_cast<uint64_t>(up ? step - half : step) * kStep + red;
             const int64_t c = c0 + line;
-            const T* w = static_cast<const T*>(up ? p.wu : p.wg) + row * (up ? p.ld_wu : p.ld_wg) + c;
+            const float* w = static_cast<const float*>(up ? p.wu : p.wg) + row * (up ? p.ld_wu : p.ld_wg) + c;
             load4(w, row < p.f ? p.k - c : 0, up ? a.wu_vectors : a.wg_vectors, v);
         });
 #pragma unroll
@@ -190,19 +181,18 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_dx_kernel(const GateArgs
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t row = m0 + thread_row(i), col = c0 + (j < 4 ? 0 : 60) + (threadIdx.x & 15u) * 4 + j;
-            if (row < p.m && col < p.k) static_cast<T*>(p.dx)[row * p.ld_dx + col] = from_float<T>(acc[i][j]);
+            if (row < p.m && col < p.k) static_cast<float*>(p.dx)[row * p.ld_dx + col] = acc[i][j];
         }
 }
 
 // ---- dWg = dG^T x (blockIdx.z = 0), dWu = dU^T x (1) ------------------------------------------------------------
 
-template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) ffn_simt_dw_kernel(const GateArgs a) {
     __shared__ __align__(16) Shared sh;
     const FfnProblem& p = a.p;
     const uint32_t f0 = blockIdx.x * kTile, c0 = blockIdx.y * kTile;
-    const T* grads = static_cast<const T*>(a.grads) + (blockIdx.z ? p.m * a.ld_grad : 0);
-    const T* x = static_cast<const T*>(p.x);
+    const float* grads = static_cast<const float*>(a.grads) + (blockIdx.z ? p.m * a.ld_grad : 0);
+    const float* x = static_cast<const float*>(p.x);
     float acc[8][8];
     product<false, false>(
         sh, acc, (p.m + kStep - 1) / kStep,
@@ -220,13 +210,13 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_simt_dw_kernel(const GateArgs
             const int64_t c = c0 + line;
             load4(x + row * p.ld_x + c, row < p.m ? p.k - c : 0, a.x_vectors, v);
         });
-    T* out = static_cast<T*>(blockIdx.z ? p.dwu : p.dwg);
+    float* out = static_cast<float*>(blockIdx.z ? p.dwu : p.dwg);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t row = f0 + thread_row(i), col = c0 + (j < 4 ? 0 : 60) + (threadIdx.x & 15u) * 4 + j;
-            if (row < p.f && col < p.k) out[row * p.ld_dw + col] = from_float<T>(acc[i][j]);
+            if (row < p.f && col < p.k) out[row * p.ld_dw + col] = acc[i][j];
         }
 }
 
@@ -245,50 +235,37 @@ GateArgs make_args(const FfnProblem& p) {
 
 uint32_t tiles(uint64_t n, uint32_t t) { return static_cast<uint32_t>((n + t - 1) / t); }
 
-template <typename T, bool BACKWARD>
+template <bool BACKWARD>
 void launch_gate(const GateArgs& a, const LaunchCtl& ctl, cudaStream_t stream) {
     const dim3 grid(tiles(a.p.m, kTile), tiles(a.p.f, 64));
-    if (a.p.activation == CDMA_ACT_RELU) ffn_simt_gate_kernel<T, CDMA_ACT_RELU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
-    else if (a.p.activation == CDMA_ACT_SILU) ffn_simt_gate_kernel<T, CDMA_ACT_SILU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
-    else ffn_simt_gate_kernel<T, CDMA_ACT_GELU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
+    if (a.p.activation == CDMA_ACT_RELU) ffn_simt_gate_kernel<CDMA_ACT_RELU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
+    else if (a.p.activation == CDMA_ACT_SILU) ffn_simt_gate_kernel<CDMA_ACT_SILU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
+    else ffn_simt_gate_kernel<CDMA_ACT_GELU, BACKWARD><<<grid, kThreads, 0, stream>>>(a, ctl);
     count_kernel_launch();
-}
-
-template <typename T>
-void launch_backward(const GateArgs& a, const LaunchCtl& ctl, cudaStream_t stream) {
-    launch_gate<T, true>(a, ctl, stream);
-    if (a.p.dx != nullptr) {
-        ffn_simt_dx_kernel<T><<<dim3(tiles(a.p.m, kTile), tiles(a.p.k, kTile)), kThreads, 0, stream>>>(a);
-        count_kernel_launch();
-    }
-    if (a.p.dwg != nullptr) {
-        ffn_simt_dw_kernel<T><<<dim3(tiles(a.p.f, kTile), tiles(a.p.k, kTile), 2), kThreads, 0, stream>>>(a);
-        count_kernel_launch();
-    }
 }
 
 }  // namespace
 
-uint64_t ffn_simt_workspace(uint64_t m, uint64_t f, uint32_t elem_size, bool backward) {
-    return backward ? 2 * m * grad_pitch(f) * elem_size : 0;
+uint64_t ffn_simt_workspace(uint64_t m, uint64_t f, bool backward) {
+    return kFfnWsHeader + (backward ? 2 * m * grad_pitch(f) * 4 : 0);
 }
 
-cudaError_t launch_ffn_simt_forward(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+cudaError_t launch_ffn_simt(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
     const GateArgs a = make_args(p);
     timing_before_launch(stream);
-    if (p.dtype == CDMA_F32) launch_gate<float, false>(a, ctl, stream);
-    else if (p.dtype == CDMA_F16) launch_gate<__half, false>(a, ctl, stream);
-    else launch_gate<__nv_bfloat16, false>(a, ctl, stream);
-    timing_after_launch(stream);
-    return cudaGetLastError();
-}
-
-cudaError_t launch_ffn_simt_backward(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
-    const GateArgs a = make_args(p);
-    timing_before_launch(stream);
-    if (p.dtype == CDMA_F32) launch_backward<float>(a, ctl, stream);
-    else if (p.dtype == CDMA_F16) launch_backward<__half>(a, ctl, stream);
-    else launch_backward<__nv_bfloat16>(a, ctl, stream);
+    if (!backward) {
+        launch_gate<false>(a, ctl, stream);
+    } else {
+        launch_gate<true>(a, ctl, stream);
+        if (p.dx != nullptr) {
+            ffn_simt_dx_kernel<<<dim3(tiles(p.m, kTile), tiles(p.k, kTile)), kThreads, 0, stream>>>(a);
+            count_kernel_launch();
+        }
+        if (p.dwg != nullptr) {
+            ffn_simt_dw_kernel<<<dim3(tiles(p.f, kTile), tiles(p.k, kTile), 2), kThreads, 0, stream>>>(a);
+            count_kernel_launch();
+        }
+    }
     timing_after_launch(stream);
     return cudaGetLastError();
 }
