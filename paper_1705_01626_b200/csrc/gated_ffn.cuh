@@ -73,11 +73,8 @@ __device__ __forceinline__ void gated_gradients(float g, float u, float dh, bool
     *dg = keep ? e * u * slope : 0.0f;
 }
 
-// 4-byte elements, on the ordinary arithmetic units (gated_ffn_simt.cu).
-uint64_t ffn_simt_workspace(uint64_t m, uint64_t f, bool backward);
-cudaError_t launch_ffn_simt(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream);
-// 2-byte elements, on the matrix units (gated_ffn_mma.cu).
-uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, bool backward);
+// The matrix products (gated_ffn_mma.cu), every type.
+uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward);
 cudaError_t launch_ffn_mma(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream);
 
 }  // namespace cdma

@@ -25,9 +25,8 @@ int check_desc(const cdma_gated_ffn_desc* d, DropoutSpec* drop) {
 uint64_t or_dense(uint64_t ld, uint64_t cols) { return ld != 0 ? ld : cols; }
 
 uint64_t workspace_of(const cdma_gated_ffn_desc& d, bool backward) {
-    const uint64_t bytes = d.dtype == CDMA_F32 ? ffn_simt_workspace(d.m, d.f, backward)
-                                               : ffn_mma_workspace(d.m, d.k, d.f, or_dense(d.ld_x, d.k), or_dense(d.ld_wg, d.k),
-                                                                   or_dense(d.ld_wu, d.k), backward);
+    const uint64_t bytes = ffn_mma_workspace(d.m, d.k, d.f, or_dense(d.ld_x, d.k), or_dense(d.ld_wg, d.k), or_dense(d.ld_wu, d.k),
+                                             d.dtype, backward);
     return (bytes + 255) & ~255ull;
 }
 
@@ -98,10 +97,6 @@ int without_kernels(const FfnProblem& p, uint64_t* h_result, cudaStream_t stream
     return result_without_kernel(p.ws, p.result_bytes, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
 }
 
-cudaError_t launch(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
-    return p.dtype == CDMA_F32 ? launch_ffn_simt(p, backward, ctl, stream) : launch_ffn_mma(p, backward, ctl, stream);
-}
-
 int64_t wait_for(int st, void* cuda_stream, const uint64_t* result) {
     if (st != CDMA_OK) return -static_cast<int64_t>(st);
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return -static_cast<int64_t>(CDMA_ERR_CUDA);
@@ -131,7 +126,7 @@ int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
     const LaunchCtl ctl = make_launch_ctl(h_result);
-    if (launch(p, false, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
+    if (launch_ffn_mma(p, false, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
     return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
 }
 
@@ -152,7 +147,7 @@ int cdma_gated_ffn_backward_async(const cdma_gated_ffn_desc* desc, const void* d
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
     const LaunchCtl ctl = make_launch_ctl(h_result);
-    if (launch(p, true, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
+    if (launch_ffn_mma(p, true, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
     return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
 }
 

@@ -23,15 +23,17 @@ inline PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
     return fn;
 }
 
-// Map of a rows x cols matrix with `ld` elements of `size` bytes from row to row, in boxes of box_cols x box_rows.
-// The start and the row stride must be multiples of 16 bytes.  Places outside the matrix read as zero.
+// Map of `planes` matrices of rows x cols elements of `size` bytes, `ld` elements from row to row and `plane` from matrix
+// to matrix, in boxes of box_cols x box_rows of one plane.  The start and the strides must be multiples of 16 bytes.
+// Places outside a matrix read as zero.
 inline bool encode_matrix_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t size, const void* p, uint64_t rows, uint64_t cols,
-                              uint64_t ld, uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+                              uint64_t ld, uint32_t planes, uint64_t plane, uint32_t box_cols, uint32_t box_rows,
+                              CUtensorMapSwizzle swizzle) {
     const auto encode = tensor_map_encoder();
     if (encode == nullptr) return false;
-    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * size};
-    const cuuint32_t box[2] = {box_cols, box_rows}, steps[2] = {1, 1};
-    return encode(map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+    const cuuint64_t dims[3] = {cols, rows, planes}, strides[2] = {ld * size, plane * size};
+    const cuuint32_t box[3] = {box_cols, box_rows, 1}, steps[3] = {1, 1, 1};
+    return encode(map, type, 3, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
