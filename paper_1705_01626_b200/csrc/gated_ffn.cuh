@@ -73,7 +73,13 @@ __device__ __forceinline__ void gated_gradients(float g, float u, float dh, bool
     *dg = keep ? e * u * slope : 0.0f;
 }
 
-// The matrix products (gated_ffn_mma.cu), every type.
+// Forward pass of few rows: of 2-byte elements with strides that TMA takes (gated_ffn_stream.cu) ...
+constexpr uint64_t kFewRows = 128;
+cudaError_t launch_ffn_stream(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
+// ... and of 4-byte elements (gated_ffn_rows.cu).
+constexpr uint64_t kFewRows4 = 8;
+cudaError_t launch_ffn_rows(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
+// Any number of rows (gated_ffn_mma.cu).
 uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward);
 cudaError_t launch_ffn_mma(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream);
 

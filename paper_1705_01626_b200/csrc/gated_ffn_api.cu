@@ -25,6 +25,7 @@ int check_desc(const cdma_gated_ffn_desc* d, DropoutSpec* drop) {
 uint64_t or_dense(uint64_t ld, uint64_t cols) { return ld != 0 ? ld : cols; }
 
 uint64_t workspace_of(const cdma_gated_ffn_desc& d, bool backward) {
+    if (!backward && d.dtype == CDMA_F32 && d.m <= kFewRows4) return kFfnWsHeader;
     const uint64_t bytes = ffn_mma_workspace(d.m, d.k, d.f, or_dense(d.ld_x, d.k), or_dense(d.ld_wg, d.k), or_dense(d.ld_wu, d.k),
                                              d.dtype, backward);
     return (bytes + 255) & ~255ull;
@@ -126,7 +127,8 @@ int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
     const LaunchCtl ctl = make_launch_ctl(h_result);
-    if (launch_ffn_mma(p, false, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
+    const cudaError_t e = p.dtype == CDMA_F32 && p.m <= kFewRows4 ? launch_ffn_rows(p, ctl, stream) : launch_ffn_mma(p, false, ctl, stream);
+    if (e != cudaSuccess) return CDMA_ERR_CUDA;
     return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
 }
 

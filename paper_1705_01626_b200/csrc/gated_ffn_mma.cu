@@ -20,8 +20,8 @@
 // the six products of planes that reach 2^-24 of the whole are six parts of one long reduction, the small ones first.
 // Six bf16 products cost less than half of what the same sum takes on the ordinary units.
 #include "gated_ffn.cuh"
+#include "gated_ffn_maps.cuh"
 #include "tcgen05.cuh"
-#include "tensor_map.h"
 
 namespace cdma {
 namespace {
@@ -565,9 +565,7 @@ __global__ void __launch_bounds__(256) join_kernel(const Product q, T* out, T* o
 
 // ---- host side -----------------------------------------------------------------------------------------------------
 
-uint64_t pitch_of(uint64_t cols) { return (cols + 63) & ~63ull; }
 uint64_t round256(uint64_t n) { return (n + 255) & ~255ull; }
-uint32_t tiles(uint64_t n, uint32_t t) { return static_cast<uint32_t>((n + t - 1) / t); }
 uint32_t planes_of(int dtype) { return dtype == CDMA_F32 ? 3 : 1; }
 bool needs_copy(uint64_t ld, uint64_t rows, int dtype) { return dtype == CDMA_F32 || (rows > 1 && ld % 8 != 0); }
 
@@ -589,8 +587,8 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
     l.dx_partial = l.wu + (needs_copy(ld_wu, f, dtype) ? round256(f * pitch_of(k) * copy) : 0);
     l.dw_partial = l.end = l.dx_partial;
     if (!backward) return l;
-    l.dx = Product{dx ? tiles(m, kTileRows) : 0, tiles(k, kProductCols), tiles(f, kStep), static_cast<uint32_t>(2 * products), 1, nullptr, pitch_of(k), m};
-    l.dw = Product{dw ? 2 * tiles(f, kTileRows) : 0, tiles(k, kProductCols), tiles(m, kStep), static_cast<uint32_t>(products), 1, nullptr, pitch_of(k), 2 * f};
+    l.dx = Product{dx ? tiles_of(m, kTileRows) : 0, tiles_of(k, kProductCols), tiles_of(f, kStep), static_cast<uint32_t>(2 * products), 1, nullptr, pitch_of(k), m};
+    l.dw = Product{dw ? 2 * tiles_of(f, kTileRows) : 0, tiles_of(k, kProductCols), tiles_of(m, kStep), static_cast<uint32_t>(products), 1, nullptr, pitch_of(k), 2 * f};
     // an even share of all steps for each pair of SMs: longer tiles are cut to about that
     uint64_t all = 0;
     for (const Product* q : {&l.dx, &l.dw}) all += static_cast<uint64_t>(q->tile_rows) * q->tile_cols * q->steps * q->parts;
@@ -602,18 +600,6 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
     l.dw_partial = l.dx_partial + (l.dx.splits > 1 && dx ? round256(l.dx.splits * l.dx.rows_partial * l.dx.ld_partial * 4) : 0);
     l.end = l.dw_partial + (l.dw.splits > 1 && dw ? round256(l.dw.splits * l.dw.rows_partial * l.dw.ld_partial * 4) : 0);
     return l;
-}
-
-struct Matrix {
-    const void* p;
-    uint64_t rows, cols, ld;
-    uint32_t planes;
-};
-// Boxes of 64 columns and `lines` rows.
-bool make_map(CUtensorMap* map, const Matrix& m, int dtype, uint32_t lines) {
-    const uint64_t ld = m.rows > 1 ? m.ld : pitch_of(m.cols);
-    return encode_matrix_map(map, dtype == CDMA_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p,
-                             m.rows, m.cols, ld, m.planes, m.rows * ld, kStep, lines, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <bool GATE, uint32_t COLS, typename T, int ACT, typename Args>
@@ -633,7 +619,7 @@ uint32_t gate_cols(uint32_t tile_rows, uint32_t f) {
     uint32_t best = 256;
     double least = 0;
     for (const auto& [cols, cost] : {std::pair<uint32_t, double>{256, 1.0}, {128, 0.58}, {64, 0.36}}) {
-        const uint64_t items = static_cast<uint64_t>(tile_rows) * tiles(f, cols / 2);
+        const uint64_t items = static_cast<uint64_t>(tile_rows) * tiles_of(f, cols / 2);
         const double t = cost * static_cast<double>((items + kPairs - 1) / kPairs);
         if (least == 0 || t < least) { least = t; best = cols; }
     }
@@ -642,8 +628,8 @@ uint32_t gate_cols(uint32_t tile_rows, uint32_t f) {
 
 template <typename T, uint32_t COLS>
 cudaError_t launch_gate(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
-    a.tile_cols = tiles(a.p.f, COLS / 2);
-    if (!make_map(&maps[2], wg, a.p.dtype, COLS / 2) || !make_map(&maps[3], wu, a.p.dtype, COLS / 2)) return cudaErrorInvalidValue;
+    a.tile_cols = tiles_of(a.p.f, COLS / 2);
+    if (!make_operand_map(&maps[2], wg, a.p.dtype, COLS / 2) || !make_operand_map(&maps[3], wu, a.p.dtype, COLS / 2)) return cudaErrorInvalidValue;
     const uint64_t items = static_cast<uint64_t>(a.tile_rows) * a.tile_cols;
     if (a.p.activation == CDMA_ACT_RELU) return launch_kernel<true, COLS, T, CDMA_ACT_RELU>(maps, a, items, ctl, stream);
     if (a.p.activation == CDMA_ACT_SILU) return launch_kernel<true, COLS, T, CDMA_ACT_SILU>(maps, a, items, ctl, stream);
@@ -658,38 +644,52 @@ cudaError_t join(const Product& q, void* out, void* out2, uint64_t ld, uint32_t 
     return cudaGetLastError();
 }
 
+// Copies the operands that need it; x, wg and wu then name what the kernels read.
 template <typename T>
-cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
-    Plan l = plan_of(p.m, p.k, p.f, p.ld_x, p.ld_wg, p.ld_wu, p.dtype, backward, p.dx != nullptr, p.dwg != nullptr);
+void prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[3], cudaStream_t stream) {
     uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
-    Matrix x{p.x, p.m, p.k, p.ld_x, 1}, wg{p.wg, p.f, p.k, p.ld_wg, 1}, wu{p.wu, p.f, p.k, p.ld_wu, 1};
+    m[0] = {p.x, p.m, p.k, p.ld_x, 1};
+    m[1] = {p.wg, p.f, p.k, p.ld_wg, 1};
+    m[2] = {p.wu, p.f, p.k, p.ld_wu, 1};
     PrepareArgs prepare{};
     int count = 0;
-    const uint64_t at[3] = {l.x, l.wg, l.wu};
-    Matrix* all[3] = {&x, &wg, &wu};
     for (int i = 0; i < 3; ++i) {
-        Matrix& o = *all[i];
+        Matrix& o = m[i];
         if (!needs_copy(o.ld, o.rows, p.dtype)) continue;
         const uint64_t pitch = pitch_of(o.cols);
-        const uint32_t groups = tiles(o.cols, 8);
+        const uint32_t groups = tiles_of(o.cols, 8);
         prepare.one[count] = {o.p, reinterpret_cast<uint16_t*>(ws + at[i]), o.ld, pitch, o.rows * pitch, static_cast<uint32_t>(o.rows),
                               static_cast<uint32_t>(o.cols), groups, o.ld % 4 == 0};
         prepare.first[count + 1] = prepare.first[count] + o.rows * groups;
         ++count;
         o = Matrix{ws + at[i], o.rows, o.cols, pitch, planes_of(p.dtype)};
     }
-    if (count != 0) {
-        for (int i = count + 1; i < 4; ++i) prepare.first[i] = prepare.first[count];
-        using Raw = typename std::conditional<sizeof(T) == 4, float, uint16_t>::type;
-        prepare_kernel<Raw><<<static_cast<uint32_t>((prepare.first[3] + 255) / 256), 256, 0, stream>>>(prepare);
-        count_kernel_launch();
+    if (count == 0) return;
+    for (int i = count + 1; i < 4; ++i) prepare.first[i] = prepare.first[count];
+    using Raw = typename std::conditional<sizeof(T) == 4, float, uint16_t>::type;
+    prepare_kernel<Raw><<<static_cast<uint32_t>((prepare.first[3] + 255) / 256), 256, 0, stream>>>(prepare);
+    count_kernel_launch();
+}
+
+template <typename T>
+cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
+    Plan l = plan_of(p.m, p.k, p.f, p.ld_x, p.ld_wg, p.ld_wu, p.dtype, backward, p.dx != nullptr, p.dwg != nullptr);
+    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    Matrix operands[3];
+    prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
+    const Matrix &x = operands[0], &wg = operands[1], &wu = operands[2];
+    if (!backward && p.dtype != CDMA_F32 && p.m <= kFewRows) {
+        FfnProblem few = p;
+        few.x = x.p, few.wg = wg.p, few.wu = wu.p;
+        few.ld_x = x.ld, few.ld_wg = wg.ld, few.ld_wu = wu.ld;
+        return launch_ffn_stream(few, ctl, stream);
     }
 
     CUtensorMap maps[4];
     const uint64_t pitch = pitch_of(p.f);
     const Matrix grads{ws + l.grads, p.m, p.f, pitch, 2 * planes_of(p.dtype)};
-    GateArgs g{p, tiles(p.m, kTileRows), 0, tiles(p.k, kStep), backward, {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
-    if (!make_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
+    GateArgs g{p, tiles_of(p.m, kTileRows), 0, tiles_of(p.k, kStep), backward, {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
+    if (!make_operand_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
     maps[1] = maps[0];
     const uint32_t cols = gate_cols(g.tile_rows, p.f);
     cudaError_t e = cols == 256   ? launch_gate<T, 256>(maps, g, wg, wu, ctl, stream)
@@ -700,8 +700,8 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     ProductsArgs a{p, l.dx, l.dw};
     a.dx.partial = reinterpret_cast<float*>(ws + l.dx_partial);
     a.dw.partial = reinterpret_cast<float*>(ws + l.dw_partial);
-    if (!make_map(&maps[0], x, p.dtype, kStep) || !make_map(&maps[1], grads, p.dtype, kStep) || !make_map(&maps[2], wg, p.dtype, kStep) ||
-        !make_map(&maps[3], wu, p.dtype, kStep))
+    if (!make_operand_map(&maps[0], x, p.dtype, kStep) || !make_operand_map(&maps[1], grads, p.dtype, kStep) || !make_operand_map(&maps[2], wg, p.dtype, kStep) ||
+        !make_operand_map(&maps[3], wu, p.dtype, kStep))
         return cudaErrorInvalidValue;
     const uint64_t items = static_cast<uint64_t>(a.dx.tile_rows) * a.dx.tile_cols * a.dx.splits +
                            static_cast<uint64_t>(a.dw.tile_rows) * a.dw.tile_cols * a.dw.splits;

@@ -1,0 +1,201 @@
+// Forward pass of the gated feed-forward block for few rows of 2-byte elements (a decoding step, a short prompt):
+// bound by the bytes of the weights, so the kernel is a stream of the weights through shared memory into the matrix
+// units, each element read once.
+//
+// The weights are operand A: 64 rows of Wg and the same 64 of Wu are the 128 rows of a tile, the rows of x, rounded
+// up to 16, its columns.  (The other way round, the tiles of gated_ffn_mma.cu, 256 rows of x would move for each few
+// rows of weights.)  A CTA's ring holds as many steps of 64 reduction elements as shared memory lets it, so that the
+// copies under way on all SMs cover the memory's latency; nothing but the two issuing threads works meanwhile.
+// Where there are fewer tiles than SMs a cluster of CTAs shares a tile's reduction; their sums meet in distributed
+// shared memory, in the order of the CTAs.
+//
+// G of an element is in another lane of tensor memory than its U, so the accumulators pass through shared memory,
+// which also turns them: neighbouring threads then store neighbouring hidden columns of one row of h.
+#include "gated_ffn.cuh"
+#include "gated_ffn_maps.cuh"
+#include "tcgen05.cuh"
+
+namespace cdma {
+namespace {
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kStep = 64;
+constexpr uint32_t kTile = 64;                             // hidden columns
+constexpr uint32_t kWeightBytes = 2 * kTile * kStep * 2;   // of a step: Wg's rows, then Wu's
+constexpr uint32_t kMaxStages = 12;
+constexpr uint32_t kPitch = 2 * kTile + 4;                 // floats per row of x in the turned accumulator
+
+struct __align__(8) Control {
+    uint64_t full[kMaxStages], empty[kMaxStages], done;
+    uint32_t tmem, gave_up;
+};
+
+struct StreamArgs {
+    FfnProblem p;
+    uint32_t steps, splits, cols, columns, stages;     // cols: rows of x, rounded up; columns: of tensor memory
+};
+
+__device__ __forceinline__ float load_from_cta(uint32_t address, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(in_cta(address, rank)) : "memory");
+    return v;
+}
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
+                                                              const __grid_constant__ CUtensorMap map_wu,
+                                                              const __grid_constant__ StreamArgs a, const LaunchCtl ctl) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Control c;
+    const uint32_t raw = shared_address(smem_raw), base = (raw + 1023u) & ~1023u;
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+    const uint32_t rank = blockIdx.x % a.splits, f0 = blockIdx.x / a.splits * kTile;
+    const uint32_t first = a.steps * rank / a.splits, last = a.steps * (rank + 1) / a.splits;
+    const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
+    const FfnProblem& p = a.p;
+
+    if (blockIdx.x == 0 && threadIdx.x == 0) init_decode_result(p.ws, ctl, p.result_bytes);
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < a.stages; ++i) {
+            mbar_init(shared_address(&c.full[i]), 1);
+            mbar_init(shared_address(&c.empty[i]), 1);
+        }
+        mbar_init(shared_address(&c.done), 1);
+        c.gave_up = 0;
+        mbar_init_fence();
+    }
+    if (warp == 2) tmem_alloc(shared_address(&c.tmem), a.columns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+
+    if (warp == 0 && lane == 0) {
+        uint32_t stage = 0, phase = 0;
+        for (uint32_t s = first; s < last; ++s) {
+            if (!mbar_wait(shared_address(&c.empty[stage]), phase ^ 1u, &c.gave_up, ctl.wait_limit_ns)) break;
+            const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
+            mbar_expect(bar, stage_bytes);
+            tma_load(dst, &map_wg, s * kStep, f0, 0, bar);
+            tma_load(dst + kWeightBytes / 2, &map_wu, s * kStep, f0, 0, bar);
+            tma_load(dst + kWeightBytes, &map_x, s * kStep, 0, 0, bar);
+            if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+        }
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t desc = mma_desc(std::is_same<T, __half>::value ? 0 : 1, false, false, 2 * kTile, a.cols);
+        uint32_t stage = 0, phase = 0;
+        bool fine = true;
+        for (uint32_t s = first; s < last; ++s) {
+            if (!(fine = mbar_wait(shared_address(&c.full[stage]), phase, &c.gave_up, ctl.wait_limit_ns))) break;
+            tcgen05_fence_after();
+            const uint32_t at = base + stage * stage_bytes;
+#pragma unroll
+            for (uint32_t i = 0; i < kStep / 16; ++i)
+                mma_single(c.tmem, operand_desc(at + 32 * i, 16, 1024), operand_desc(at + kWeightBytes + 32 * i, 16, 1024), desc, s != first || i != 0);
+            mma_commit_single(shared_address(&c.empty[stage]));
+            if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (fine) mma_commit_single(shared_address(&c.done));
+    }
+    __syncwarp();
+    const bool fine = mbar_wait(shared_address(&c.done), 0, &c.gave_up, ctl.wait_limit_ns);
+    tcgen05_fence_after();
+    __syncwarp();
+    // every copy has been consumed: the ring now takes the accumulator, a row of it for each row of x
+    float* turned = reinterpret_cast<float*>(smem_raw + (base - raw));
+    if (fine) {
+        for (uint32_t col = 16 * (warp >> 2); col < a.cols; col += 32) {
+            uint32_t v[16];
+            tmem_load16(c.tmem + ((warp & 3u) * 32u << 16) + col, v);
+            tmem_load_wait();
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) turned[(col + i) * kPitch + (warp & 3u) * 32 + lane] = __uint_as_float(v[i]);
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*static_cast<volatile uint32_t*>(&c.gave_up)) {
+        if (threadIdx.x == 0) report_decode_error(p.ws, ctl, CDMA_ERR_TIMEOUT);
+        for (uint32_t i = 0; i < 1000; ++i) __nanosleep(1000);      // what is still under way ends within microseconds
+    }
+    if (a.splits > 1) cluster_sync();
+
+    // the CTAs of a cluster take turns at the rows of x
+    const uint32_t rows = (p.m + a.splits - 1 - rank) / a.splits, at = base;
+    for (uint32_t e = threadIdx.x; e < rows * kTile; e += kThreads) {
+        const uint32_t row = rank + a.splits * (e / kTile), j = e % kTile;
+        if (f0 + j >= p.f) continue;
+        float g = 0.0f, u = 0.0f;
+        if (a.splits == 1) {
+            g = turned[row * kPitch + j];
+            u = turned[row * kPitch + kTile + j];
+        } else {
+            for (uint32_t s = 0; s < a.splits; ++s) {
+                g += load_from_cta(at + (row * kPitch + j) * 4, s);
+                u += load_from_cta(at + (row * kPitch + kTile + j) * 4, s);
+            }
+        }
+        const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row, (f0 + j) >> 3) >> (j & 7u) : 1u;
+        static_cast<T*>(p.h)[row * p.ld_h + f0 + j] = from_float<T>(gated_value<ACT, true>(g, u, keep & 1u, p.drop.scale));
+    }
+    __syncthreads();
+    if (a.splits > 1) cluster_sync();      // nobody leaves while its sums are read
+    if (warp == 2) tmem_free(c.tmem, a.columns);
+}
+
+template <typename T, int ACT>
+cudaError_t launch_kernel(const CUtensorMap (&maps)[3], const StreamArgs& a, uint32_t tiles, uint32_t smem, const LaunchCtl& ctl, cudaStream_t stream) {
+    auto kernel = ffn_stream_kernel<T, ACT>;
+    const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), 232448 - sizeof(Control) - 64);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(tiles * a.splits);
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim = {a.splits, 1, 1};
+    config.attrs = &cluster;
+    config.numAttrs = 1;
+    count_kernel_launch();
+    return cudaLaunchKernelEx(&config, kernel, maps[0], maps[1], maps[2], a, ctl);
+}
+
+template <typename T>
+cudaError_t launch_type(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+    StreamArgs a{};
+    a.p = p;
+    a.steps = tiles_of(p.k, kStep);
+    a.cols = (p.m + 15) & ~15u;
+    a.columns = 32;
+    while (a.columns < a.cols) a.columns *= 2;
+    // CTAs for at most two rounds of SMs, each with steps enough to fill its ring once
+    const uint32_t tiles = tiles_of(p.f, kTile);
+    a.splits = 1;
+    while (a.splits < 8 && tiles * a.splits * 2 <= 296 && a.steps / (a.splits * 2) >= 4) a.splits *= 2;
+    // one CTA to an SM may take all of its shared memory, else two share it
+    const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
+    const uint32_t room = tiles * a.splits <= 148 ? 220 * 1024 : 108 * 1024;
+    a.stages = room / stage_bytes < kMaxStages ? room / stage_bytes : kMaxStages;
+    const uint32_t least = tiles_of(a.cols * kPitch * 4, stage_bytes);      // room for the turned accumulator
+    const uint32_t most = tiles_of(a.steps, a.splits);
+    if (a.stages > most) a.stages = most;
+    const uint32_t ring = (a.stages > least ? a.stages : least) * stage_bytes;
+    CUtensorMap maps[3];
+    if (!make_operand_map(&maps[0], {p.x, p.m, p.k, p.ld_x, 1}, p.dtype, a.cols) ||
+        !make_operand_map(&maps[1], {p.wg, p.f, p.k, p.ld_wg, 1}, p.dtype, kTile) ||
+        !make_operand_map(&maps[2], {p.wu, p.f, p.k, p.ld_wu, 1}, p.dtype, kTile))
+        return cudaErrorInvalidValue;
+    const uint32_t smem = ring + 1024;
+    if (p.activation == CDMA_ACT_RELU) return launch_kernel<T, CDMA_ACT_RELU>(maps, a, tiles, smem, ctl, stream);
+    if (p.activation == CDMA_ACT_SILU) return launch_kernel<T, CDMA_ACT_SILU>(maps, a, tiles, smem, ctl, stream);
+    return launch_kernel<T, CDMA_ACT_GELU>(maps, a, tiles, smem, ctl, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_ffn_stream(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+    return p.dtype == CDMA_F16 ? launch_type<__half>(p, ctl, stream) : launch_type<__nv_bfloat16>(p, ctl, stream);
+}
+
+}  // namespace cdma
