@@ -1,0 +1,747 @@
+// The gated feed-forward block on the matrix units (tcgen05).
+//
+//   gate kernel      G and U of 256 rows and up to 128 hidden columns: A = x, B = the tile's rows of Wg next to those
+//                    of Wu, so that an accumulator holds G and U of the same elements and its reader has both at hand.
+//                    The reader writes h (forward), or dG and dU (backward, after reading dh).
+//   products kernel  256 x 256 tiles of dx (A = dG then dU, B = Wg then Wu, one reduction over both) and of dWg and
+//                    dWu (A = dG^T or dU^T, B = x), in one launch: both only need dG and dU.
+//
+// A pair of CTAs on two SMs shares one tile (cta_group::2): each holds half of A's and half of B's rows, and the
+// accumulator of its half of the output rows.  In the gate kernel one CTA brings Wg's rows and the other Wu's.
+// Operands arrive by TMA in 128-byte swizzled steps of 64 reduction elements through a ring; one thread issues the
+// matrix instructions; eight warps read the finished accumulator while the other of two collects the next tile.
+// Operands whose rows, not their reduction, are contiguous in memory (B of dx, both of dW) are taken as they lie, by
+// the descriptors' major bits: nothing is transposed.
+//
+// Sizes that are no multiple of a tile need nothing: TMA fills with zeros outside the matrix and the readers store
+// what is inside.  TMA wants 16-byte row strides; an operand with another stride is copied first (prepare_kernel).
+//
+// 4-byte elements: each operand is split into three bf16 planes (x = high + middle + low, 8 bits each: all 24), and
+// the six products of planes that reach 2^-24 of the whole are six parts of one long reduction, the small ones first.
+// Six bf16 products cost less than half of what the same sum takes on the ordinary units.
+#pragma once
+
+#include "gated_ffn.cuh"
+#include "gated_ffn_maps.cuh"
+#include "tcgen05.cuh"
+
+namespace cdma {
+namespace mma {
+
+constexpr uint32_t kPairs = 74;                      // pairs of SMs
+constexpr uint32_t kStep = 64;                       // reduction elements per step: 128 bytes
+constexpr uint32_t kHalfBytes = 128 * kStep * 2;     // one CTA's half of A: 128 rows
+constexpr uint32_t kTileRows = 256;
+constexpr uint32_t kReaderWarps = 8;
+constexpr uint32_t kThreads = 32 * (4 + kReaderWarps);
+constexpr uint32_t kBand = 16;                       // tile rows that are walked together
+constexpr uint32_t kMaxStages = 9;
+
+template <typename T> struct Planes { static constexpr uint32_t count = 1, products = 1; };
+template <> struct Planes<float> { static constexpr uint32_t count = 3, products = 6; };
+// Planes of A and of B in the parts of the reduction (4 bits each, the first part lowest).
+constexpr uint32_t kPlaneOfA = 0x010120u, kPlaneOfB = 0x001102u;
+
+// Warp-private block of shared memory through which 32 x 32 elements turn: a thread has a row of them in registers,
+// memory wants neighbouring threads on neighbouring columns.  Rows are padded by 16 bytes: no bank conflicts.
+template <typename T> constexpr uint32_t kTurnPitch = 32 * sizeof(T) + 16;
+
+struct __align__(8) Control {
+    uint64_t full[kMaxStages], empty[kMaxStages], done[2], free_[2];
+    uint32_t tmem, gave_up;
+};
+
+// A kernel's shape: GATE or products, columns of a tile, and what follows from the type.
+template <bool GATE, bool BACKWARD, uint32_t COLS, typename T>
+struct Config {
+    static constexpr bool kGate = GATE, kBackward = BACKWARD;
+    static constexpr uint32_t kCols = COLS;
+    static constexpr uint32_t kStageBytes = kHalfBytes + COLS / 2 * kStep * 2;
+    static constexpr uint32_t kTurnBlocks = GATE && BACKWARD && sizeof(T) == 2 ? 2 : 1;     // dG and dU are turned side by side
+    static constexpr uint32_t kTurnBytes = kReaderWarps * kTurnBlocks * 32 * kTurnPitch<T>;
+    // as many steps as fit beside the turning blocks and the barriers (227 KB)
+    static constexpr uint32_t kFit = (232448 - 1024 - sizeof(Control) - kTurnBytes) / kStageBytes;
+    static constexpr uint32_t kStages = kFit < kMaxStages ? kFit : kMaxStages;
+    static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + kTurnBytes + sizeof(Control);
+    // two accumulators; 4-byte elements have their running sums beside them
+    static constexpr uint32_t kTmemCols = sizeof(T) == 4 ? 4 * COLS : 2 * COLS;
+    static_assert(kTmemCols <= 512, "tensor memory has 512 columns");
+};
+
+struct Gradients {      // dG then dU, each in its planes: `m` rows of `ld` 2-byte elements per plane
+    uint16_t* at;
+    uint64_t ld;
+};
+struct GateArgs {
+    FfnProblem p;
+    uint32_t tile_rows, tile_cols, steps;
+    Gradients grads;
+};
+// Tiles of one product.  With splits > 1 each tile's reduction is cut into that many items, which leave sums in 32
+// bits for the joining kernel: where there are fewer tiles than pairs of SMs.
+struct Product {
+    uint32_t tile_rows, tile_cols, steps, parts, splits;
+    float* partial;
+    uint64_t ld_partial, rows_partial;
+};
+struct ProductsArgs {
+    FfnProblem p;
+    Product dx, dw;
+};
+
+// What a pair of CTAs does at one time: an output tile and a range of its reduction.
+struct Item {
+    bool dw, second;          // products: dW; of dWu
+    uint32_t row, col;        // of the tile
+    uint32_t first, last;     // steps, counted through the parts
+    uint32_t steps, split;
+    uint32_t small;           // steps of the small products of planes, which come first
+};
+
+// Tiles in bands of kBand tile rows, down a band's column first: the tiles that run at one time then share few rows
+// of either operand, which stay in L2.
+__device__ __forceinline__ void place(uint32_t tile, uint32_t tile_rows, uint32_t tile_cols, uint32_t* row, uint32_t* col) {
+    const uint32_t per_band = kBand * tile_cols;
+    const uint32_t band = tile / per_band, rest = tile % per_band;
+    const uint32_t height = min(kBand, tile_rows - band * kBand);
+    *row = band * kBand + rest % height;
+    *col = rest / height;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t items_of(const GateArgs& a) { return a.tile_rows * a.tile_cols; }
+template <typename T>
+__device__ __forceinline__ Item item_of(const GateArgs& a, uint32_t index) {
+    Item it{};
+    place(index, a.tile_rows, a.tile_cols, &it.row, &it.col);
+    it.steps = a.steps;
+    it.last = a.steps * Planes<T>::products;
+    it.small = it.last - a.steps;
+    return it;
+}
+__device__ __forceinline__ uint32_t items_of(const Product& q) { return q.tile_rows * q.tile_cols * q.splits; }
+template <typename T>
+__device__ __forceinline__ uint32_t items_of(const ProductsArgs& a) { return items_of(a.dx) + items_of(a.dw); }
+template <typename T>
+__device__ __forceinline__ Item item_of(const ProductsArgs& a, uint32_t index) {
+    Item it{};
+    it.dw = index >= items_of(a.dx);
+    const Product& q = it.dw ? a.dw : a.dx;
+    const uint32_t i = it.dw ? index - items_of(a.dx) : index, tiles = q.tile_rows * q.tile_cols;
+    it.split = i / tiles;
+    place(i % tiles, q.tile_rows, q.tile_cols, &it.row, &it.col);
+    const uint64_t total = static_cast<uint64_t>(q.steps) * q.parts;
+    it.first = static_cast<uint32_t>(total * it.split / q.splits);
+    it.last = static_cast<uint32_t>(total * (it.split + 1) / q.splits);
+    it.steps = q.steps;
+    it.small = static_cast<uint32_t>(total) - (it.dw ? 1 : 2) * q.steps;
+    if (it.dw && it.row >= q.tile_rows / 2) {      // the upper half of the tile rows are dWu's
+        it.second = true;
+        it.row -= q.tile_rows / 2;
+    }
+    return it;
+}
+
+// ---- between registers and memory --------------------------------------------------------------------------------
+
+// The warp's turning block to or from memory: 32 rows of 32 elements, `at` the first, `rows` and `cols` what exists.
+// `at` + `ld` decide between 16-byte accesses and single elements; what does not exist is read as zero.
+template <typename T, bool STORE>
+__device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, int64_t rows, int64_t cols) {
+    constexpr uint32_t kPitch = kTurnPitch<T>, kVectors = 32 * sizeof(T) / 16, kRowsAtOnce = 32 / kVectors;
+    const uint32_t lane = lane_id();
+    __syncwarp();
+    if (cols >= 32 && ((reinterpret_cast<uintptr_t>(at) | ld * sizeof(T)) & 15u) == 0) {
+        const uint32_t first = lane / kVectors, vector = lane % kVectors;
+#pragma unroll
+        for (uint32_t i = 0; i < kVectors; ++i) {
+            const uint32_t r = i * kRowsAtOnce + first;
+            uint4* there = reinterpret_cast<uint4*>(at + r * ld + vector * (16 / sizeof(T)));
+            uint4* here = reinterpret_cast<uint4*>(turn + r * kPitch + 16 * vector);
+            if (STORE) { if (r < rows) *there = *here; }
+            else *here = r < rows ? __ldg(there) : make_uint4(0, 0, 0, 0);
+        }
+    } else {
+#pragma unroll 8
+        for (uint32_t r = 0; r < 32; ++r) {
+            T* here = reinterpret_cast<T*>(turn + r * kPitch + lane * sizeof(T));
+            const bool exists = r < rows && lane < cols;
+            if (STORE) { if (exists) at[r * ld + lane] = *here; }
+            else *here = exists ? at[r * ld + lane] : from_float<T>(0.0f);
+        }
+    }
+    __syncwarp();
+}
+
+// The three bf16 planes of a float, cut off so that the two upper ones never round up to infinity.  What is not
+// finite goes into the first plane alone.
+__device__ __forceinline__ void split3(float v, uint32_t (&planes)[3]) {
+    const uint32_t bits = __float_as_uint(v);
+    const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+    const uint32_t high = finite || (bits & 0x007fffffu) == 0 ? bits & 0xffff0000u : 0x7fc00000u;
+    const float rest = finite ? v - __uint_as_float(high) : 0.0f;
+    const uint32_t middle = __float_as_uint(rest) & 0xffff0000u;
+    planes[0] = high >> 16;
+    planes[1] = middle >> 16;
+    planes[2] = pack2<__nv_bfloat16>(rest - __uint_as_float(middle), 0.0f) & 0xffffu;
+}
+
+// Eight neighbouring elements of the thread's row of the turning block.
+template <typename T>
+__device__ __forceinline__ void put8(uint8_t* turn, uint32_t col, const float (&v)[8]) {
+    uint4* to = reinterpret_cast<uint4*>(turn + lane_id() * kTurnPitch<T> + col * sizeof(T));
+    if constexpr (sizeof(T) == 4) {
+        to[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        to[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    } else {
+        to[0] = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void get8(const uint8_t* turn, uint32_t col, float (&v)[8]) {
+    const uint4* from = reinterpret_cast<const uint4*>(turn + lane_id() * kTurnPitch<T> + col * sizeof(T));
+    const uint4 q = from[0];
+    if constexpr (sizeof(T) == 4) {
+        const uint4 r = from[1];
+        const uint32_t w[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+    } else {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack2<T>(w[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+}
+
+// Eight neighbouring elements of a gradient into its bf16 planes of the workspace.
+__device__ __forceinline__ void store_planes8(uint16_t* to, uint64_t plane, const float (&v)[8]) {
+    uint32_t words[3][4];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        uint32_t lo[3], hi[3];
+        split3(v[i], lo);
+        split3(v[i + 1], hi);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) words[j][i / 2] = lo[j] | hi[j] << 16;
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4*>(to + j * plane) = make_uint4(words[j][0], words[j][1], words[j][2], words[j][3]);
+}
+
+// 32 hidden columns of the warp's 32 rows: h, or dG and dU; G at tensor-memory place `g`, U at `u`.  Eight columns at
+// a time in a rolled loop: unrolled over all columns the code does not fit the instruction cache, and the first tile
+// of a launch, often its only one, waited for instructions most of the time (GELU: 37,000 cycles for 32 columns).
+template <typename T, int ACT, bool BACKWARD>
+__device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, uint32_t row, uint32_t col, uint32_t g, uint32_t u) {
+    const FfnProblem& p = a.p;
+    constexpr bool kFast = sizeof(T) == 2;
+    uint8_t* second = turn + 32 * kTurnPitch<T>;
+    const int64_t rows = static_cast<int64_t>(p.m) - row;
+    uint16_t* grads = a.grads.at + (row + lane_id()) * a.grads.ld + col;
+    const uint64_t plane = static_cast<uint64_t>(p.m) * a.grads.ld;
+#pragma unroll 1
+    for (uint32_t c = 0; c < 32; c += 8) {
+        uint32_t gw[8], uw[8];
+        tmem_load8(g + c, gw);
+        tmem_load8(u + c, uw);
+        const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row + lane_id(), (col + c) >> 3) : 0xffu;
+        float dh[8], first[8], other[8];
+        if (BACKWARD) get8<T>(turn, c, dh);
+        tmem_load_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float gv = __uint_as_float(gw[j]), uv = __uint_as_float(uw[j]);
+            const bool kept = (keep >> j) & 1u;
+            if (BACKWARD) gated_gradients<ACT, kFast>(gv, uv, dh[j], kept, p.drop.scale, &first[j], &other[j]);
+            else first[j] = gated_value<ACT, kFast>(gv, uv, kept, p.drop.scale);
+        }
+        if constexpr (BACKWARD && sizeof(T) == 4) {
+            if (lane_id() < rows && col < p.f) {
+                store_planes8(grads + c, plane, first);
+                store_planes8(grads + 3 * plane + c, plane, other);
+            }
+        } else {
+            put8<T>(turn, c, first);
+            if (BACKWARD) put8<T>(second, c, other);
+        }
+    }
+    if (row >= p.m || col >= p.f) return;       // the same for the whole warp
+    if constexpr (!BACKWARD) {
+        move_block<T, true>(turn, static_cast<T*>(p.h) + row * p.ld_h + col, p.ld_h, rows, static_cast<int64_t>(p.f) - col);
+    } else if constexpr (sizeof(T) == 2) {      // the pitch there is a multiple of 64 elements: 32 columns always fit
+        T* to = reinterpret_cast<T*>(a.grads.at) + row * a.grads.ld + col;
+        move_block<T, true>(turn, to, a.grads.ld, rows, 32);
+        move_block<T, true>(second, to + plane, a.grads.ld, rows, 32);
+    }
+}
+
+// ---- the three roles of a CTA --------------------------------------------------------------------------------------
+
+template <uint32_t DEPTH>
+struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++stage == DEPTH) { stage = 0; phase ^= 1u; }
+    }
+};
+
+// The matrix unit cuts its sums off instead of rounding them, which shows in 32 bits: the sums of 4-byte elements are
+// taken out every few steps and added on the ordinary units.  The small products of planes, 2^-8 of the whole, are one
+// such stretch.  (1000 x 1024 x 2752 fp32: error 2.2e-6 in one stretch, the plain sum in 32 bits has 0.9e-6.)
+constexpr uint32_t kStretch = 4;
+template <typename T>
+__device__ __forceinline__ uint32_t end_of_stretch(const Item& it, uint32_t s) {
+    if (sizeof(T) == 2) return it.last;
+    return min(it.last, s < it.small ? it.small : s + kStretch);
+}
+
+// One warp per CTA, one of its threads: brings this CTA's halves of A and B; the bytes of both CTAs are counted by the
+// first one's barrier.  (The whole warp walks the loop: what one thread computes alone cannot live in the uniform
+// registers that the copies and the matrix instructions take their operands from.)
+template <typename C, typename T, typename Args>
+__device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map_x, const CUtensorMap* map_g, const CUtensorMap* map_wg,
+                                           const CUtensorMap* map_wu, uint32_t base, Control& c, const LaunchCtl& ctl) {
+    const uint32_t rank = cluster_rank(), items = items_of<T>(a);
+    const uint32_t full = in_cta(shared_address(&c.full[0]), 0), own_full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
+    Ring<C::kStages> ring;
+    bool fine = true;
+    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
+        const Item it = item_of<T>(a, index);
+        const uint32_t row = it.row * kTileRows + rank * 128;
+        const uint32_t col = C::kGate ? it.col * (C::kCols / 2) : it.col * C::kCols + rank * (C::kCols / 2);
+        uint32_t part = it.first / it.steps, r = it.first % it.steps * kStep;
+        for (uint32_t s = it.first; s < it.last; ++s) {
+            if (!(fine = mbar_wait(empty + 8 * ring.stage, ring.phase ^ 1u, &c.gave_up, ctl.wait_limit_ns))) break;
+            const uint32_t bar = full + 8 * ring.stage;
+            const uint32_t dst_a = base + ring.stage * C::kStageBytes, dst_b = dst_a + kHalfBytes;
+            // the products of planes are the outer parts; dx has a half for G and one for U in each
+            const bool up = !C::kGate && !it.dw && (part & 1u);
+            const uint32_t product = !C::kGate && !it.dw ? part >> 1 : part;
+            const uint32_t plane_a = sizeof(T) == 4 ? kPlaneOfA >> (4 * product) & 15u : 0;
+            const uint32_t plane_b = sizeof(T) == 4 ? kPlaneOfB >> (4 * product) & 15u : 0;
+            const uint32_t of_g = ((it.dw ? it.second : up) ? Planes<T>::count : 0) + plane_a;
+            if (elect_one()) {
+                if (rank == 0) mbar_expect(own_full + 8 * ring.stage, 2 * C::kStageBytes);
+                if constexpr (C::kGate) {
+                    tma_load_pair(dst_a, map_x, r, row, plane_a, bar);
+                    if (rank == 0) tma_load_pair(dst_b, map_wg, r, col, plane_b, bar);
+                    else tma_load_pair(dst_b, map_wu, r, col, plane_b, bar);
+                } else if (!it.dw) {
+                    tma_load_pair(dst_a, map_g, r, row, of_g, bar);
+                    tma_load_pair(dst_a + kHalfBytes / 2, map_g, r, row + 64, of_g, bar);
+#pragma unroll
+                    for (uint32_t i = 0; i < C::kCols / 128; ++i) {
+                        if (up) tma_load_pair(dst_b + i * 8192, map_wu, col + 64 * i, r, plane_b, bar);
+                        else tma_load_pair(dst_b + i * 8192, map_wg, col + 64 * i, r, plane_b, bar);
+                    }
+                } else {
+                    tma_load_pair(dst_a, map_g, row, r, of_g, bar);
+                    tma_load_pair(dst_a + kHalfBytes / 2, map_g, row + 64, r, of_g, bar);
+#pragma unroll
+                    for (uint32_t i = 0; i < C::kCols / 128; ++i) tma_load_pair(dst_b + i * 8192, map_x, col + 64 * i, r, plane_b, bar);
+                }
+            }
+            __syncwarp();
+            ring.next();
+            r += kStep;
+            if (r >= it.steps * kStep) { r = 0; ++part; }
+        }
+    }
+    // the last steps' releases have arrived here before this CTA's shared memory goes
+    for (uint32_t i = 0; fine && i < C::kStages; ++i) {
+        fine = mbar_wait(empty + 8 * ring.stage, ring.phase ^ 1u, &c.gave_up, ctl.wait_limit_ns);
+        ring.next();
+    }
+}
+
+// One warp of the pair, one of its threads: issues the matrix instructions.  A reduction-contiguous operand's rows lie
+// 128 bytes apart, eight rows in 1024 bytes, and a sub-step of 16 is 32 bytes on; of the other kind a block of 64 rows
+// is 8192 bytes, eight reduction lines are 1024, and a sub-step is 2048 bytes on.
+template <typename C, typename T, typename Args>
+__device__ __forceinline__ void run_issuer(const Args& a, uint32_t base, Control& c, const LaunchCtl& ctl) {
+    constexpr uint32_t kFormat = std::is_same<T, __half>::value ? 0 : 1;
+    constexpr uint32_t kDesc = mma_desc(kFormat, false, !C::kGate, kTileRows, C::kCols);
+    constexpr uint32_t kDescDw = mma_desc(kFormat, true, true, kTileRows, C::kCols);
+    const uint32_t items = items_of<T>(a), tmem = c.tmem;
+    const uint32_t full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
+    Ring<C::kStages> ring;
+    uint32_t n = 0;
+    bool fine = true;
+    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
+        const Item it = item_of<T>(a, index);
+        const bool a_rows = !C::kGate && it.dw;
+        const uint32_t desc = a_rows ? kDescDw : kDesc;
+        const uint64_t like_a = a_rows ? operand_desc(0, 8192, 1024) : operand_desc(0, 16, 1024);
+        const uint64_t like_b = C::kGate ? operand_desc(0, 16, 1024) : operand_desc(0, 8192, 1024);
+        const uint32_t step_a = a_rows ? 2048 >> 4 : 32 >> 4;
+        constexpr uint32_t step_b = C::kGate ? 32 >> 4 : 2048 >> 4;
+        for (uint32_t s = it.first; fine && s < it.last; ++n) {
+            const uint32_t end = end_of_stretch<T>(it, s), acc = n & 1u, to = tmem + acc * C::kCols;
+            if (!(fine = mbar_wait_cluster(shared_address(&c.free_[acc]), ((n >> 1) & 1u) ^ 1u, &c.gave_up, ctl.wait_limit_ns))) break;
+            tcgen05_fence_after();
+            bool more = false;      // the first instruction overwrites
+            for (; s < end; ++s) {
+                if (!(fine = mbar_wait(full + 8 * ring.stage, ring.phase, &c.gave_up, ctl.wait_limit_ns))) break;
+                tcgen05_fence_after();
+                const uint32_t at = (base + ring.stage * C::kStageBytes) >> 4;
+                if (elect_one()) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kStep / 16; ++i)
+                        mma_pair(to, like_a + at + i * step_a, like_b + at + (kHalfBytes >> 4) + i * step_b, desc, more || i != 0);
+                    mma_commit_pair(empty + 8 * ring.stage);
+                }
+                __syncwarp();
+                more = true;
+                ring.next();
+            }
+            if (fine && elect_one()) mma_commit_pair(shared_address(&c.done[acc]));
+            __syncwarp();
+        }
+    }
+}
+
+// Eight warps: quarters of the accumulator's rows, every other block of 32 columns.
+template <typename C, typename T, int ACT, typename Args>
+__device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Control& c, const LaunchCtl& ctl) {
+    const uint32_t warp = (threadIdx.x >> 5) - 4, quarter = warp & 3u, half = warp >> 2, rank = cluster_rank(), lane = lane_id();
+    uint8_t* turn = turns + warp * C::kTurnBlocks * 32 * kTurnPitch<T>;
+    const uint32_t items = items_of<T>(a), free0 = in_cta(shared_address(&c.free_[0]), 0);
+    const FfnProblem& p = a.p;
+    const uint32_t tmem = c.tmem + (quarter * 32u << 16), sums = tmem + 2 * C::kCols;
+    constexpr uint32_t kBlocks = C::kGate ? C::kCols / 64 : C::kCols / 32;
+    uint32_t n = 0;
+    bool fine = true;
+    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
+        const Item it = item_of<T>(a, index);
+        const uint32_t row = it.row * kTileRows + rank * 128 + quarter * 32;      // the warp's first
+        auto load_dh = [&](uint32_t i) {
+            const uint32_t col = it.col * (C::kCols / 2) + i * 32;
+            if (row < p.m && col < p.f)
+                move_block<T, false>(turn, const_cast<T*>(static_cast<const T*>(p.dh)) + row * p.ld_h + col, p.ld_h,
+                                     static_cast<int64_t>(p.m) - row, static_cast<int64_t>(p.f) - col);
+        };
+        if (C::kBackward && half < kBlocks) load_dh(half);      // while the accumulator is still collected
+        uint32_t from = tmem;
+        for (uint32_t s = it.first; s < it.last; ++n) {
+            const uint32_t end = end_of_stretch<T>(it, s), acc = n & 1u;
+            if (!(fine = mbar_wait(shared_address(&c.done[acc]), (n >> 1) & 1u, &c.gave_up, ctl.wait_limit_ns))) break;
+            tcgen05_fence_after();
+            __syncwarp();
+            from = tmem + acc * C::kCols;
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll 1
+                for (uint32_t i = half; i < C::kCols / 32; i += 2) {
+                    // blocks of G and of U alternate between the warps as the gate's reader takes them
+                    const uint32_t at = i * 32;
+                    uint32_t v[32], w[32];
+                    tmem_load32(from + at, v);
+                    if (s != it.first) tmem_load32(sums + at, w);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = s != it.first ? __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(w[j])) : v[j];
+                    tmem_store32(sums + at, v);
+                }
+                tmem_store_wait();
+                tcgen05_fence_before();
+                if (lane == 0) mbar_arrive_cluster(free0 + 8 * acc);
+            }
+            s = end;
+        }
+        if (!fine) break;
+        if constexpr (sizeof(T) == 4) from = sums;
+        if constexpr (C::kGate) {
+#pragma unroll 1
+            for (uint32_t i = half; i < kBlocks; i += 2) {
+                if (C::kBackward && i != half) load_dh(i);
+                finish_gate<T, ACT, C::kBackward>(a, turn, row, it.col * (C::kCols / 2) + i * 32, from + i * 32, from + C::kCols / 2 + i * 32);
+            }
+        } else {
+            const Product& q = it.dw ? a.dw : a.dx;
+            T* out = static_cast<T*>(!it.dw ? p.dx : it.second ? p.dwu : p.dwg);
+            const uint64_t ld = it.dw ? p.ld_dw : p.ld_dx;
+            const uint32_t rows = it.dw ? p.f : p.m;
+#pragma unroll 1
+            for (uint32_t i = half; i < kBlocks; i += 2) {
+                const uint32_t col = it.col * C::kCols + i * 32;
+                uint32_t v[32];
+                tmem_load32(from + i * 32, v);
+                tmem_load_wait();
+                if (row >= rows || col >= p.k) continue;
+                if (q.splits > 1) {
+                    if (row + lane < rows) {
+                        float* to = q.partial + (it.split * q.rows_partial + (it.second ? rows : 0) + row + lane) * q.ld_partial + col;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) reinterpret_cast<uint4*>(to)[j] = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        const float eight[8] = {__uint_as_float(v[j]), __uint_as_float(v[j + 1]), __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]),
+                                                __uint_as_float(v[j + 4]), __uint_as_float(v[j + 5]), __uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])};
+                        put8<T>(turn, j, eight);
+                    }
+                    move_block<T, true>(turn, out + row * ld + col, ld, static_cast<int64_t>(rows) - row, static_cast<int64_t>(p.k) - col);
+                }
+            }
+        }
+        __syncwarp();
+        if constexpr (sizeof(T) == 2) {
+            tcgen05_fence_before();
+            if (lane == 0) mbar_arrive_cluster(free0 + 8 * ((n - 1) & 1u));
+        }
+    }
+}
+
+template <typename C, typename T, int ACT, typename Args>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g,
+               const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
+               const __grid_constant__ Args a, const LaunchCtl ctl) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = shared_address(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* turns = smem_raw + (base - raw) + C::kStages * C::kStageBytes;
+    Control& c = *reinterpret_cast<Control*>(turns + C::kTurnBytes);
+    const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
+
+    if (C::kGate && blockIdx.x == 0 && threadIdx.x == 0) init_decode_result(a.p.ws, ctl, a.p.result_bytes);
+    if (warp == 0 && lane == 0) {
+        for (uint32_t i = 0; i < C::kStages; ++i) {
+            mbar_init(shared_address(&c.full[i]), 1);
+            mbar_init(shared_address(&c.empty[i]), 1);
+        }
+        for (uint32_t i = 0; i < 2; ++i) {
+            mbar_init(shared_address(&c.done[i]), 1);
+            mbar_init(shared_address(&c.free_[i]), 2 * kReaderWarps);
+        }
+        c.gave_up = 0;
+        mbar_init_fence();
+    } else if (warp == 3 && lane == 0) {
+        tma_prefetch_map(&map_x);
+        tma_prefetch_map(&map_g);
+        tma_prefetch_map(&map_wg);
+        tma_prefetch_map(&map_wu);
+    }
+    if (warp == 2) tmem_alloc_pair(shared_address(&c.tmem), C::kTmemCols);
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tcgen05_fence_after();
+
+    if (warp == 0) run_loader<C, T>(a, &map_x, &map_g, &map_wg, &map_wu, base, c, ctl);
+    else if (warp == 1 && cluster_rank() == 0) run_issuer<C, T>(a, base, c, ctl);
+    else if (warp >= 4) run_readers<C, T, ACT>(a, turns, c, ctl);
+
+    __syncwarp();
+    __syncthreads();
+    if (*static_cast<volatile uint32_t*>(&c.gave_up)) {
+        if (threadIdx.x == 0) report_decode_error(a.p.ws, ctl, CDMA_ERR_TIMEOUT);
+        // copies and matrix instructions that are still under way end within microseconds
+        for (uint32_t i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 2) tmem_free_pair(c.tmem, C::kTmemCols);
+}
+
+// ---- operands that TMA or the matrix units cannot take as they are -------------------------------------------------
+
+// Copies of up to three operands: 2-byte elements with a row stride that is a multiple of 64 elements, or the planes
+// of 4-byte elements.  A thread makes eight neighbouring elements.
+struct PrepareArgs {
+    struct One {
+        const void* from;
+        uint16_t* to;
+        uint64_t ld_from, ld_to, plane;
+        uint32_t rows, cols, groups, vectors;      // groups of eight per row
+    } one[3];
+    uint64_t first[4];      // numbers of the operands' first groups, then the end
+};
+template <typename T>
+__global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
+    const uint64_t n = blockIdx.x * 256ull + threadIdx.x;
+    if (n >= a.first[3]) return;
+    const int which = n >= a.first[2] ? 2 : n >= a.first[1] ? 1 : 0;
+    const PrepareArgs::One& o = a.one[which];
+    const uint64_t local = n - a.first[which];
+    const uint64_t row = local >> 32 ? local / o.groups : static_cast<uint32_t>(local) / o.groups;
+    const uint32_t col = static_cast<uint32_t>(local - row * o.groups) * 8;
+    const T* from = static_cast<const T*>(o.from) + row * o.ld_from + col;
+    uint16_t* to = o.to + row * o.ld_to + col;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < o.cols ? from[i] : 0;
+        *reinterpret_cast<uint4*>(to) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    } else {
+        float v[8];
+        if (o.vectors && col + 8 <= o.cols) {
+            *reinterpret_cast<float4*>(v) = reinterpret_cast<const float4*>(from)[0];
+            *reinterpret_cast<float4*>(v + 4) = reinterpret_cast<const float4*>(from)[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = col + i < o.cols ? from[i] : 0.0f;
+        }
+        uint32_t planes[3][4];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            uint32_t lo[3], hi[3];
+            split3(v[i], lo);
+            split3(v[i + 1], hi);
+#pragma unroll
+            for (int j = 0; j < 3; ++j) planes[j][i / 2] = lo[j] | hi[j] << 16;
+        }
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            *reinterpret_cast<uint4*>(to + j * o.plane) = make_uint4(planes[j][0], planes[j][1], planes[j][2], planes[j][3]);
+    }
+}
+
+// Adds the splits' sums in their order and rounds once.
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(const Product q, T* out, T* out2, uint64_t ld, uint32_t rows, uint32_t cols) {
+    const uint32_t groups = (cols + 3) / 4;
+    const uint64_t n = blockIdx.x * 256ull + threadIdx.x;
+    const uint64_t row = n / groups;
+    const uint32_t col = static_cast<uint32_t>(n % groups) * 4;
+    if (row >= q.rows_partial) return;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t s = 0; s < q.splits; ++s) {
+        const float4 v = *reinterpret_cast<const float4*>(q.partial + (s * q.rows_partial + row) * q.ld_partial + col);
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    T* to = (row < rows ? out + row * ld : out2 + (row - rows) * ld) + col;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < cols) to[i] = from_float<T>(v[i]);
+}
+
+// ---- launching -------------------------------------------------------------------------------------------------------
+
+uint32_t planes_of(int dtype);
+bool needs_copy(uint64_t ld, uint64_t rows, int dtype);
+
+// Where things lie in the workspace behind the result words, and how the products are cut.
+struct Plan {
+    uint64_t grads, x, wg, wu, dx_partial, dw_partial, end;
+    Product dx, dw;
+};
+Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward, bool dx, bool dw);
+
+// Columns of a products tile: the running sums of 4-byte elements take the other half of tensor memory.
+constexpr uint32_t product_cols(uint64_t size) { return size == 4 ? 128 : 256; }
+// Hidden columns of a gate tile of 2-byte elements, times two.
+uint32_t gate_cols(uint32_t tile_rows, uint32_t f);
+
+template <typename C, typename T, int ACT, typename Args>
+cudaError_t launch_kernel(const CUtensorMap (&maps)[4], const Args& a, uint64_t items, const LaunchCtl& ctl, cudaStream_t stream) {
+    auto kernel = ffn_mma_kernel<C, T, ACT, Args>;
+    const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), C::kSharedBytes);
+    if (e != cudaSuccess) return e;
+    const uint32_t pairs = items < kPairs ? static_cast<uint32_t>(items) : kPairs;
+    kernel<<<2 * pairs, kThreads, C::kSharedBytes, stream>>>(maps[0], maps[1], maps[2], maps[3], a, ctl);
+    count_kernel_launch();
+    return cudaGetLastError();
+}
+
+template <typename T, bool BACKWARD, uint32_t COLS>
+cudaError_t launch_gate_of(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
+    using C = Config<true, BACKWARD, COLS, T>;
+    a.tile_cols = tiles_of(a.p.f, COLS / 2);
+    if (!make_operand_map(&maps[2], wg, a.p.dtype, COLS / 2) || !make_operand_map(&maps[3], wu, a.p.dtype, COLS / 2)) return cudaErrorInvalidValue;
+    const uint64_t items = static_cast<uint64_t>(a.tile_rows) * a.tile_cols;
+    if (a.p.activation == CDMA_ACT_RELU) return launch_kernel<C, T, CDMA_ACT_RELU>(maps, a, items, ctl, stream);
+    if (a.p.activation == CDMA_ACT_SILU) return launch_kernel<C, T, CDMA_ACT_SILU>(maps, a, items, ctl, stream);
+    return launch_kernel<C, T, CDMA_ACT_GELU>(maps, a, items, ctl, stream);
+}
+template <typename T, bool BACKWARD>
+cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
+    if constexpr (sizeof(T) == 4) {
+        return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
+    } else {
+        const uint32_t cols = gate_cols(a.tile_rows, a.p.f);
+        if (cols == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
+        if (cols == 128) return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
+        return launch_gate_of<T, BACKWARD, 64>(maps, a, wg, wu, ctl, stream);
+    }
+}
+
+template <typename T>
+cudaError_t join(const Product& q, void* out, void* out2, uint64_t ld, uint32_t rows, uint32_t cols, cudaStream_t stream) {
+    const uint64_t n = q.rows_partial * ((cols + 3) / 4);
+    join_kernel<T><<<static_cast<uint32_t>((n + 255) / 256), 256, 0, stream>>>(q, static_cast<T*>(out), static_cast<T*>(out2), ld, rows, cols);
+    count_kernel_launch();
+    return cudaGetLastError();
+}
+
+// Copies the operands that need it; x, wg and wu then name what the kernels read.
+template <typename T>
+void prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[3], cudaStream_t stream) {
+    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    m[0] = {p.x, p.m, p.k, p.ld_x, 1};
+    m[1] = {p.wg, p.f, p.k, p.ld_wg, 1};
+    m[2] = {p.wu, p.f, p.k, p.ld_wu, 1};
+    PrepareArgs prepare{};
+    int count = 0;
+    for (int i = 0; i < 3; ++i) {
+        Matrix& o = m[i];
+        if (!needs_copy(o.ld, o.rows, p.dtype)) continue;
+        const uint64_t pitch = pitch_of(o.cols);
+        const uint32_t groups = tiles_of(o.cols, 8);
+        prepare.one[count] = {o.p, reinterpret_cast<uint16_t*>(ws + at[i]), o.ld, pitch, o.rows * pitch, static_cast<uint32_t>(o.rows),
+                              static_cast<uint32_t>(o.cols), groups, o.ld % 4 == 0};
+        prepare.first[count + 1] = prepare.first[count] + o.rows * groups;
+        ++count;
+        o = Matrix{ws + at[i], o.rows, o.cols, pitch, planes_of(p.dtype)};
+    }
+    if (count == 0) return;
+    for (int i = count + 1; i < 4; ++i) prepare.first[i] = prepare.first[count];
+    using Raw = typename std::conditional<sizeof(T) == 4, float, uint16_t>::type;
+    prepare_kernel<Raw><<<static_cast<uint32_t>((prepare.first[3] + 255) / 256), 256, 0, stream>>>(prepare);
+    count_kernel_launch();
+}
+
+template <typename T>
+cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
+    Plan l = plan_of(p.m, p.k, p.f, p.ld_x, p.ld_wg, p.ld_wu, p.dtype, backward, p.dx != nullptr, p.dwg != nullptr);
+    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    Matrix operands[3];
+    prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
+    const Matrix &x = operands[0], &wg = operands[1], &wu = operands[2];
+    if (!backward && p.dtype != CDMA_F32 && p.m <= kFewRows) {
+        FfnProblem few = p;
+        few.x = x.p, few.wg = wg.p, few.wu = wu.p;
+        few.ld_x = x.ld, few.ld_wg = wg.ld, few.ld_wu = wu.ld;
+        return launch_ffn_stream(few, ctl, stream);
+    }
+
+    CUtensorMap maps[4];
+    const uint64_t pitch = pitch_of(p.f);
+    const Matrix grads{ws + l.grads, p.m, p.f, pitch, 2 * planes_of(p.dtype)};
+    GateArgs g{p, tiles_of(p.m, kTileRows), 0, tiles_of(p.k, kStep), {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
+    if (!make_operand_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
+    maps[1] = maps[0];
+    cudaError_t e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
+    if (e != cudaSuccess || !backward) return e;
+
+    ProductsArgs a{p, l.dx, l.dw};
+    a.dx.partial = reinterpret_cast<float*>(ws + l.dx_partial);
+    a.dw.partial = reinterpret_cast<float*>(ws + l.dw_partial);
+    if (!make_operand_map(&maps[0], x, p.dtype, kStep) || !make_operand_map(&maps[1], grads, p.dtype, kStep) || !make_operand_map(&maps[2], wg, p.dtype, kStep) ||
+        !make_operand_map(&maps[3], wu, p.dtype, kStep))
+        return cudaErrorInvalidValue;
+    const uint64_t items = static_cast<uint64_t>(a.dx.tile_rows) * a.dx.tile_cols * a.dx.splits +
+                           static_cast<uint64_t>(a.dw.tile_rows) * a.dw.tile_cols * a.dw.splits;
+    e = launch_kernel<Config<false, false, product_cols(sizeof(T)), T>, T, 0>(maps, a, items, ctl, stream);
+    if (e == cudaSuccess && p.dx != nullptr && a.dx.splits > 1) e = join<T>(a.dx, p.dx, nullptr, p.ld_dx, p.m, p.k, stream);
+    if (e == cudaSuccess && p.dwg != nullptr && a.dw.splits > 1) e = join<T>(a.dw, p.dwg, p.dwu, p.ld_dw, p.f, p.k, stream);
+    return e;
+}
+
+}  // namespace mma
+}  // namespace cdma

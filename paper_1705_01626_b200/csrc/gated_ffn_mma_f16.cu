@@ -1,0 +1,9 @@
+#include "gated_ffn_mma.cuh"
+
+namespace cdma {
+namespace mma {
+
+template cudaError_t launch_all<__half>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);
+
+}  // namespace mma
+}  // namespace cdma

@@ -65,36 +65,47 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
         mbar_init_fence();
     }
     if (warp == 2) tmem_alloc(shared_address(&c.tmem), a.columns);
+    if (threadIdx.x == 96) {
+        tma_prefetch_map(&map_wg);
+        tma_prefetch_map(&map_wu);
+        tma_prefetch_map(&map_x);
+    }
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         uint32_t stage = 0, phase = 0;
         for (uint32_t s = first; s < last; ++s) {
             if (!mbar_wait(shared_address(&c.empty[stage]), phase ^ 1u, &c.gave_up, ctl.wait_limit_ns)) break;
             const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
-            mbar_expect(bar, stage_bytes);
-            tma_load(dst, &map_wg, s * kStep, f0, 0, bar);
-            tma_load(dst + kWeightBytes / 2, &map_wu, s * kStep, f0, 0, bar);
-            tma_load(dst + kWeightBytes, &map_x, s * kStep, 0, 0, bar);
+            if (elect_one()) {
+                mbar_expect(bar, stage_bytes);
+                tma_load(dst, &map_wg, s * kStep, f0, 0, bar);
+                tma_load(dst + kWeightBytes / 2, &map_wu, s * kStep, f0, 0, bar);
+                tma_load(dst + kWeightBytes, &map_x, s * kStep, 0, 0, bar);
+            }
+            __syncwarp();
             if (++stage == a.stages) { stage = 0; phase ^= 1u; }
         }
-    } else if (warp == 1 && lane == 0) {
-        const uint32_t desc = mma_desc(std::is_same<T, __half>::value ? 0 : 1, false, false, 2 * kTile, a.cols);
+    } else if (warp == 1) {
+        const uint32_t desc = mma_desc(std::is_same<T, __half>::value ? 0 : 1, false, false, 2 * kTile, a.cols), tmem = c.tmem;
         uint32_t stage = 0, phase = 0;
         bool fine = true;
         for (uint32_t s = first; s < last; ++s) {
             if (!(fine = mbar_wait(shared_address(&c.full[stage]), phase, &c.gave_up, ctl.wait_limit_ns))) break;
             tcgen05_fence_after();
             const uint32_t at = base + stage * stage_bytes;
+            if (elect_one()) {
 #pragma unroll
-            for (uint32_t i = 0; i < kStep / 16; ++i)
-                mma_single(c.tmem, operand_desc(at + 32 * i, 16, 1024), operand_desc(at + kWeightBytes + 32 * i, 16, 1024), desc, s != first || i != 0);
-            mma_commit_single(shared_address(&c.empty[stage]));
+                for (uint32_t i = 0; i < kStep / 16; ++i)
+                    mma_single(tmem, operand_desc(at + 32 * i, 16, 1024), operand_desc(at + kWeightBytes + 32 * i, 16, 1024), desc, s != first || i != 0);
+                mma_commit_single(shared_address(&c.empty[stage]));
+            }
+            __syncwarp();
             if (++stage == a.stages) { stage = 0; phase ^= 1u; }
         }
-        if (fine) mma_commit_single(shared_address(&c.done));
+        if (fine && elect_one()) mma_commit_single(shared_address(&c.done));
     }
     __syncwarp();
     const bool fine = mbar_wait(shared_address(&c.done), 0, &c.gave_up, ctl.wait_limit_ns);

@@ -40,27 +40,45 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// One thread of a warp whose threads are all here, always the same one.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t chosen;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(chosen));
+    return chosen != 0;
+}
+// CLUSTER: for arrivals of another CTA's threads (what TMA and the matrix unit signal needs no wider scope).
+template <bool CLUSTER>
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (CLUSTER)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// Waits for the phase; false when the limit passed or another thread of the CTA gave up (*gave_up, in shared memory).
+// A whole warp waits for the phase; false, for all of its threads, when the limit passed for one of them or another
+// warp of the CTA gave up (*gave_up, in shared memory).
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint64_t limit_ns) {
-    if (mbar_try(bar, parity)) return true;
+    bool done = mbar_try<CLUSTER>(bar, parity);
     uint64_t t0 = 0;
-    for (uint32_t polls = 1; polls < kWaitLimitPolls; ++polls) {
-        if (mbar_try(bar, parity)) return true;
-        if ((polls & 63u) == 0) {
-            if (*gave_up) return false;
+    for (uint32_t polls = 1; !done && polls < kWaitLimitPolls; ++polls) {
+        done = mbar_try<CLUSTER>(bar, parity);
+        if (!done && (polls & 63u) == 0) {
+            if (*gave_up) break;
             const uint64_t t = global_timer_ns();
             if (t0 == 0) t0 = t;
             else if (t - t0 > limit_ns) break;
         }
     }
-    *gave_up = 1;
-    return false;
+    done = __all_sync(0xffffffffu, done);
+    if (!done) *gave_up = 1;
+    return done;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint64_t limit_ns) {
+    return mbar_wait<true>(bar, parity, gave_up, limit_ns);
 }
 
 // ---- TMA -----------------------------------------------------------------------------------------------------------
@@ -146,6 +164,20 @@ __device__ __forceinline__ void tmem_load32(uint32_t tmem, uint32_t (&v)[32]) {
                    "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(tmem));
 }
+__device__ __forceinline__ void tmem_load8(uint32_t tmem, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(tmem));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t tmem, const uint32_t (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+                 ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+                   "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+                   "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+                   "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(tmem) : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 }  // namespace cdma
