@@ -260,18 +260,20 @@ def cdma_zvc_relu_backward_async(d_src, src_bytes, d_table, n, dtype, layout, d_
                                                   _vp(h_result)))
 
 
+# The operators are called every few microseconds: addresses go through as the numbers they are (0 is NULL).
+
 def cdma_dropout(d_x, ld_x, d_residual, ld_residual, rows, cols, dtype, p, seed, sequence, d_y, ld_y,
                  cuda_stream=0) -> int:
     """y = residual + (kept ? x * scale : 0); the mask is a function of (seed, sequence, row, col).
     d_residual may be 0.  Only enqueues; returns a status."""
-    return int(lib().cdma_dropout(_vp(d_x), ld_x, _vp(d_residual), ld_residual, rows, cols, dtype, p, seed, sequence,
-                                  _vp(d_y), ld_y, _vp(cuda_stream)))
+    return int(lib().cdma_dropout(d_x, ld_x, d_residual, ld_residual, rows, cols, dtype, p, seed, sequence,
+                                  d_y, ld_y, cuda_stream))
 
 
 def cdma_dropout_backward(d_dy, ld_dy, rows, cols, dtype, p, seed, sequence, d_dx, ld_dx, cuda_stream=0) -> int:
     """dx = kept ? dy * scale : 0 with the forward call's p, seed and sequence.  Only enqueues; returns a status."""
-    return int(lib().cdma_dropout_backward(_vp(d_dy), ld_dy, rows, cols, dtype, p, seed, sequence, _vp(d_dx), ld_dx,
-                                           _vp(cuda_stream)))
+    return int(lib().cdma_dropout_backward(d_dy, ld_dy, rows, cols, dtype, p, seed, sequence, d_dx, ld_dx,
+                                           cuda_stream))
 
 
 def cdma_gated_ffn_workspace_bytes(desc, backward: int) -> int:
@@ -280,29 +282,29 @@ def cdma_gated_ffn_workspace_bytes(desc, backward: int) -> int:
 
 def cdma_gated_ffn_forward(desc, d_x, d_wg, d_wu, d_h, d_workspace, workspace_bytes, cuda_stream=0) -> int:
     """h = dropout(act(x Wg^T) * (x Wu^T)).  Returns the bytes of h, or a negative status."""
-    return int(lib().cdma_gated_ffn_forward(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_h), _vp(d_workspace),
-                                            workspace_bytes, _vp(cuda_stream)))
+    return int(lib().cdma_gated_ffn_forward(desc, d_x, d_wg, d_wu, d_h, d_workspace,
+                                            workspace_bytes, cuda_stream))
 
 
 def cdma_gated_ffn_forward_async(desc, d_x, d_wg, d_wu, d_h, d_workspace, workspace_bytes, cuda_stream,
                                  h_result) -> int:
-    return int(lib().cdma_gated_ffn_forward_async(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_h), _vp(d_workspace),
-                                                  workspace_bytes, _vp(cuda_stream), _vp(h_result)))
+    return int(lib().cdma_gated_ffn_forward_async(desc, d_x, d_wg, d_wu, d_h, d_workspace,
+                                                  workspace_bytes, cuda_stream, h_result))
 
 
 def cdma_gated_ffn_backward(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace, workspace_bytes,
                             cuda_stream=0) -> int:
     """Gradients of the block from its inputs and dh; d_dx, or d_dwg and d_dwu, may be 0.
     Returns the bytes of the gradients written, or a negative status."""
-    return int(lib().cdma_gated_ffn_backward(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_dh), _vp(d_dx), _vp(d_dwg),
-                                             _vp(d_dwu), _vp(d_workspace), workspace_bytes, _vp(cuda_stream)))
+    return int(lib().cdma_gated_ffn_backward(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg,
+                                             d_dwu, d_workspace, workspace_bytes, cuda_stream))
 
 
 def cdma_gated_ffn_backward_async(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace, workspace_bytes,
                                   cuda_stream, h_result) -> int:
-    return int(lib().cdma_gated_ffn_backward_async(desc, _vp(d_x), _vp(d_wg), _vp(d_wu), _vp(d_dh), _vp(d_dx),
-                                                   _vp(d_dwg), _vp(d_dwu), _vp(d_workspace), workspace_bytes,
-                                                   _vp(cuda_stream), _vp(h_result)))
+    return int(lib().cdma_gated_ffn_backward_async(desc, d_x, d_wg, d_wu, d_dh, d_dx,
+                                                   d_dwg, d_dwu, d_workspace, workspace_bytes,
+                                                   cuda_stream, h_result))
 
 
 def cdma_ctx_create(pinned_bytes: int, device_staging_bytes: int):

@@ -1,5 +1,6 @@
 // Dropout with a mask that is never stored: y = residual + (kept ? x * scale : 0), and its backward pass, which is
 // the same call on the gradient.  The mask function is in dropout.cuh, the contract in include/cdma.h.
+#include "chained_launch.cuh"
 #include "dropout.cuh"
 #include "elements.cuh"
 #include "operand_checks.h"
@@ -53,6 +54,8 @@ __device__ __forceinline__ T one_element(const Args<T>& a, uint64_t ix, uint64_t
 template <typename T, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const Args<T> a) {
     constexpr int kVecs = sizeof(T) * 8 / 16;
+    let_next_start();
+    wait_for_previous();
     const uint32_t q = blockIdx.x * kThreads + threadIdx.x;
     if (q >= a.blocks) return;
     const uint32_t r = divide(q, a.per_row);
@@ -96,6 +99,8 @@ __global__ void __launch_bounds__(kThreads) dropout_ragged_kernel(const Args<T> 
         block = q - r * a.per_row.divisor;
         keep = dropout_keep8(a.drop, a.first_row + r, block);
     }
+    let_next_start();
+    wait_for_previous();
     const uint32_t sub = lane_id() & 7u;
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
@@ -119,18 +124,17 @@ cudaError_t launch(const void* x, uint64_t ld_x, const void* residual, uint64_t 
     // a launch numbers its blocks in 32 bits, whole rows at a time
     const uint64_t most_rows = 0x80000000ull / a.per_row.divisor > 0 ? 0x80000000ull / a.per_row.divisor : 1;
     timing_before_launch(stream);
-    for (uint64_t row = 0; row < rows; row += most_rows) {
+    cudaError_t e = cudaSuccess;
+    for (uint64_t row = 0; e == cudaSuccess && row < rows; row += most_rows) {
         const uint64_t n = rows - row < most_rows ? rows - row : most_rows;
         a.first_row = static_cast<uint32_t>(row);
         a.blocks = static_cast<uint32_t>(n * a.per_row.divisor);
         const uint32_t grid = static_cast<uint32_t>((static_cast<uint64_t>(a.blocks) + kThreads - 1) / kThreads);
-        if (!vectors) dropout_ragged_kernel<T><<<grid, kThreads, 0, stream>>>(a);
-        else if (residual != nullptr) dropout_kernel<T, true><<<grid, kThreads, 0, stream>>>(a);
-        else dropout_kernel<T, false><<<grid, kThreads, 0, stream>>>(a);
-        count_kernel_launch();
+        e = launch_chained(!vectors ? dropout_ragged_kernel<T> : residual != nullptr ? dropout_kernel<T, true> : dropout_kernel<T, false>,
+                           grid, kThreads, 0, 0, stream, a);
     }
     timing_after_launch(stream);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace

@@ -21,6 +21,7 @@
 // Six bf16 products cost less than half of what the same sum takes on the ordinary units.
 #pragma once
 
+#include "chained_launch.cuh"
 #include "gated_ffn.cuh"
 #include "gated_ffn_maps.cuh"
 #include "tcgen05.cuh"
@@ -243,15 +244,22 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
     const int64_t rows = static_cast<int64_t>(p.m) - row;
     uint16_t* grads = a.grads.at + (row + lane_id()) * a.grads.ld + col;
     const uint64_t plane = static_cast<uint64_t>(p.m) * a.grads.ld;
+    uint32_t next_g[8], next_u[8];
+    tmem_load8(g, next_g);
+    tmem_load8(u, next_u);
 #pragma unroll 1
     for (uint32_t c = 0; c < 32; c += 8) {
-        uint32_t gw[8], uw[8];
-        tmem_load8(g + c, gw);
-        tmem_load8(u + c, uw);
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row + lane_id(), (col + c) >> 3) : 0xffu;
         float dh[8], first[8], other[8];
         if (BACKWARD) get8<T>(turn, c, dh);
+        uint32_t gw[8], uw[8];
         tmem_load_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { gw[j] = next_g[j]; uw[j] = next_u[j]; }
+        if (c + 8 < 32) {
+            tmem_load8(g + c + 8, next_g);
+            tmem_load8(u + c + 8, next_u);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float gv = __uint_as_float(gw[j]), uv = __uint_as_float(uw[j]);
@@ -381,7 +389,7 @@ __device__ __forceinline__ void run_issuer(const Args& a, uint32_t base, Control
         constexpr uint32_t step_b = C::kGate ? 32 >> 4 : 2048 >> 4;
         for (uint32_t s = it.first; fine && s < it.last; ++n) {
             const uint32_t end = end_of_stretch<T>(it, s), acc = n & 1u, to = tmem + acc * C::kCols;
-            if (!(fine = mbar_wait_cluster(shared_address(&c.free_[acc]), ((n >> 1) & 1u) ^ 1u, &c.gave_up, ctl.wait_limit_ns))) break;
+            if (!(fine = mbar_wait(shared_address(&c.free_[acc]), ((n >> 1) & 1u) ^ 1u, &c.gave_up, ctl.wait_limit_ns))) break;
             tcgen05_fence_after();
             bool more = false;      // the first instruction overwrites
             for (; s < end; ++s) {
@@ -464,12 +472,16 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             T* out = static_cast<T*>(!it.dw ? p.dx : it.second ? p.dwu : p.dwg);
             const uint64_t ld = it.dw ? p.ld_dw : p.ld_dx;
             const uint32_t rows = it.dw ? p.f : p.m;
+            uint32_t next[32];
+            tmem_load32(from + half * 32, next);
 #pragma unroll 1
             for (uint32_t i = half; i < kBlocks; i += 2) {
                 const uint32_t col = it.col * C::kCols + i * 32;
                 uint32_t v[32];
-                tmem_load32(from + i * 32, v);
                 tmem_load_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = next[j];
+                if (i + 2 < kBlocks) tmem_load32(from + (i + 2) * 32, next);
                 if (row >= rows || col >= p.k) continue;
                 if (q.splits > 1) {
                     if (row + lane < rows) {
@@ -507,7 +519,6 @@ ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     Control& c = *reinterpret_cast<Control*>(turns + C::kTurnBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
 
-    if (C::kGate && blockIdx.x == 0 && threadIdx.x == 0) init_decode_result(a.p.ws, ctl, a.p.result_bytes);
     if (warp == 0 && lane == 0) {
         for (uint32_t i = 0; i < C::kStages; ++i) {
             mbar_init(shared_address(&c.full[i]), 1);
@@ -530,6 +541,9 @@ ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     __syncthreads();
     cluster_sync();
     tcgen05_fence_after();
+    let_next_start();
+    wait_for_previous();
+    if (C::kGate && blockIdx.x == 0 && threadIdx.x == 96) init_decode_result(a.p.ws, ctl, a.p.result_bytes);
 
     if (warp == 0) run_loader<C, T>(a, &map_x, &map_g, &map_wg, &map_wu, base, c, ctl);
     else if (warp == 1 && cluster_rank() == 0) run_issuer<C, T>(a, base, c, ctl);
@@ -564,6 +578,8 @@ struct PrepareArgs {
 template <typename T>
 __global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
     const uint64_t n = blockIdx.x * 256ull + threadIdx.x;
+    let_next_start();
+    wait_for_previous();
     if (n >= a.first[3]) return;
     const int which = n >= a.first[2] ? 2 : n >= a.first[1] ? 1 : 0;
     const PrepareArgs::One& o = a.one[which];
@@ -604,6 +620,8 @@ __global__ void __launch_bounds__(256) prepare_kernel(const PrepareArgs a) {
 // Adds the splits' sums in their order and rounds once.
 template <typename T>
 __global__ void __launch_bounds__(256) join_kernel(const Product q, T* out, T* out2, uint64_t ld, uint32_t rows, uint32_t cols) {
+    let_next_start();
+    wait_for_previous();
     const uint32_t groups = (cols + 3) / 4;
     const uint64_t n = blockIdx.x * 256ull + threadIdx.x;
     const uint64_t row = n / groups;
@@ -644,9 +662,7 @@ cudaError_t launch_kernel(const CUtensorMap (&maps)[4], const Args& a, uint64_t 
     const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), C::kSharedBytes);
     if (e != cudaSuccess) return e;
     const uint32_t pairs = items < kPairs ? static_cast<uint32_t>(items) : kPairs;
-    kernel<<<2 * pairs, kThreads, C::kSharedBytes, stream>>>(maps[0], maps[1], maps[2], maps[3], a, ctl);
-    count_kernel_launch();
-    return cudaGetLastError();
+    return launch_chained(kernel, 2 * pairs, kThreads, C::kSharedBytes, 0, stream, maps[0], maps[1], maps[2], maps[3], a, ctl);
 }
 
 template <typename T, bool BACKWARD, uint32_t COLS>
@@ -674,14 +690,13 @@ cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix&
 template <typename T>
 cudaError_t join(const Product& q, void* out, void* out2, uint64_t ld, uint32_t rows, uint32_t cols, cudaStream_t stream) {
     const uint64_t n = q.rows_partial * ((cols + 3) / 4);
-    join_kernel<T><<<static_cast<uint32_t>((n + 255) / 256), 256, 0, stream>>>(q, static_cast<T*>(out), static_cast<T*>(out2), ld, rows, cols);
-    count_kernel_launch();
-    return cudaGetLastError();
+    return launch_chained(join_kernel<T>, static_cast<uint32_t>((n + 255) / 256), 256, 0, 0, stream, q, static_cast<T*>(out),
+                          static_cast<T*>(out2), ld, rows, cols);
 }
 
 // Copies the operands that need it; x, wg and wu then name what the kernels read.
 template <typename T>
-void prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[3], cudaStream_t stream) {
+cudaError_t prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[3], cudaStream_t stream) {
     uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
     m[0] = {p.x, p.m, p.k, p.ld_x, 1};
     m[1] = {p.wg, p.f, p.k, p.ld_wg, 1};
@@ -699,11 +714,10 @@ void prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[
         ++count;
         o = Matrix{ws + at[i], o.rows, o.cols, pitch, planes_of(p.dtype)};
     }
-    if (count == 0) return;
+    if (count == 0) return cudaSuccess;
     for (int i = count + 1; i < 4; ++i) prepare.first[i] = prepare.first[count];
     using Raw = typename std::conditional<sizeof(T) == 4, float, uint16_t>::type;
-    prepare_kernel<Raw><<<static_cast<uint32_t>((prepare.first[3] + 255) / 256), 256, 0, stream>>>(prepare);
-    count_kernel_launch();
+    return launch_chained(prepare_kernel<Raw>, static_cast<uint32_t>((prepare.first[3] + 255) / 256), 256, 0, 0, stream, prepare);
 }
 
 template <typename T>
@@ -711,7 +725,8 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     Plan l = plan_of(p.m, p.k, p.f, p.ld_x, p.ld_wg, p.ld_wu, p.dtype, backward, p.dx != nullptr, p.dwg != nullptr);
     uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
     Matrix operands[3];
-    prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
+    cudaError_t e = prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
+    if (e != cudaSuccess) return e;
     const Matrix &x = operands[0], &wg = operands[1], &wu = operands[2];
     if (!backward && p.dtype != CDMA_F32 && p.m <= kFewRows) {
         FfnProblem few = p;
@@ -726,7 +741,7 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     GateArgs g{p, tiles_of(p.m, kTileRows), 0, tiles_of(p.k, kStep), {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
     if (!make_operand_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
     maps[1] = maps[0];
-    cudaError_t e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
+    e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
     if (e != cudaSuccess || !backward) return e;
 
     ProductsArgs a{p, l.dx, l.dw};

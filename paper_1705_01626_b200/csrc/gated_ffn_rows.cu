@@ -12,6 +12,7 @@
 // 4-byte elements are split in two tf32 parts (11 bits each, rounded to nearest) and multiplied as high*high +
 // high*low + low*high.  The matrix unit cuts its sums off instead of rounding them, so a sum of a few instructions
 // is added to the running one on the ordinary units: without that the loss grows with the reduction's length.
+#include "chained_launch.cuh"
 #include "gated_ffn.cuh"
 
 namespace cdma {
@@ -99,6 +100,8 @@ __global__ void __launch_bounds__(kThreads) ffn_rows_kernel(const FfnProblem p, 
     __shared__ float sums[kWarps][TILES][4][32];
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id(), row8 = lane >> 2, quad = lane & 3u;
     const uint32_t f0 = blockIdx.x * 8;
+    let_next_start();
+    wait_for_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) init_decode_result(p.ws, ctl, p.result_bytes);
 
     const bool feature = f0 + row8 < p.f;
@@ -157,36 +160,27 @@ __global__ void __launch_bounds__(kThreads) ffn_rows_kernel(const FfnProblem p, 
 }
 
 template <typename T, int TILES, bool VECTORS>
-void launch_act(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+cudaError_t launch_act(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
     const uint32_t grid = (p.f + 7) / 8;
-    if (p.activation == CDMA_ACT_RELU) ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_RELU><<<grid, kThreads, 0, stream>>>(p, ctl);
-    else if (p.activation == CDMA_ACT_SILU) ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_SILU><<<grid, kThreads, 0, stream>>>(p, ctl);
-    else ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_GELU><<<grid, kThreads, 0, stream>>>(p, ctl);
-    count_kernel_launch();
+    if (p.activation == CDMA_ACT_RELU) return launch_chained(ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_RELU>, grid, kThreads, 0, 0, stream, p, ctl);
+    if (p.activation == CDMA_ACT_SILU) return launch_chained(ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_SILU>, grid, kThreads, 0, 0, stream, p, ctl);
+    return launch_chained(ffn_rows_kernel<T, TILES, VECTORS, CDMA_ACT_GELU>, grid, kThreads, 0, 0, stream, p, ctl);
 }
-template <typename T, bool VECTORS>
-void launch_tiles(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
-    if (p.m <= 8) launch_act<T, 1, VECTORS>(p, ctl, stream);
-    else if (p.m <= 16) launch_act<T, 2, VECTORS>(p, ctl, stream);
-    else if (p.m <= 32) launch_act<T, 4, VECTORS>(p, ctl, stream);
-    else launch_act<T, 8, VECTORS>(p, ctl, stream);
-}
-template <typename T>
-void launch_type(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
-    constexpr uint64_t kCount = 16 / sizeof(T);
-    if (p.ld_wg % kCount == 0 && p.ld_wu % kCount == 0 && (p.ld_x % kCount == 0 || p.m == 1)) launch_tiles<T, true>(p, ctl, stream);
-    else launch_tiles<T, false>(p, ctl, stream);
+template <bool VECTORS>
+cudaError_t launch_tiles(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+    if (p.m <= 8) return launch_act<float, 1, VECTORS>(p, ctl, stream);
+    if (p.m <= 16) return launch_act<float, 2, VECTORS>(p, ctl, stream);
+    return launch_act<float, 4, VECTORS>(p, ctl, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_ffn_rows(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
     timing_before_launch(stream);
-    if (p.dtype == CDMA_F32) launch_type<float>(p, ctl, stream);
-    else if (p.dtype == CDMA_F16) launch_type<__half>(p, ctl, stream);
-    else launch_type<__nv_bfloat16>(p, ctl, stream);
+    const bool vectors = p.ld_wg % 4 == 0 && p.ld_wu % 4 == 0 && (p.ld_x % 4 == 0 || p.m == 1);
+    const cudaError_t e = vectors ? launch_tiles<true>(p, ctl, stream) : launch_tiles<false>(p, ctl, stream);
     timing_after_launch(stream);
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace cdma

@@ -11,6 +11,7 @@
 //
 // G of an element is in another lane of tensor memory than its U, so the accumulators pass through shared memory,
 // which also turns them: neighbouring threads then store neighbouring hidden columns of one row of h.
+#include "chained_launch.cuh"
 #include "gated_ffn.cuh"
 #include "gated_ffn_maps.cuh"
 #include "tcgen05.cuh"
@@ -54,7 +55,6 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
     const FfnProblem& p = a.p;
 
-    if (blockIdx.x == 0 && threadIdx.x == 0) init_decode_result(p.ws, ctl, p.result_bytes);
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < a.stages; ++i) {
             mbar_init(shared_address(&c.full[i]), 1);
@@ -73,6 +73,9 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
+    let_next_start();
+    wait_for_previous();
+    if (blockIdx.x == 0 && threadIdx.x == 128) init_decode_result(p.ws, ctl, p.result_bytes);
 
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -158,18 +161,7 @@ cudaError_t launch_kernel(const CUtensorMap (&maps)[3], const StreamArgs& a, uin
     auto kernel = ffn_stream_kernel<T, ACT>;
     const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), 232448 - sizeof(Control) - 64);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(tiles * a.splits);
-    config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    cudaLaunchAttribute cluster{};
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim = {a.splits, 1, 1};
-    config.attrs = &cluster;
-    config.numAttrs = 1;
-    count_kernel_launch();
-    return cudaLaunchKernelEx(&config, kernel, maps[0], maps[1], maps[2], a, ctl);
+    return launch_chained(kernel, tiles * a.splits, kThreads, smem, a.splits, stream, maps[0], maps[1], maps[2], a, ctl);
 }
 
 template <typename T>

@@ -37,8 +37,10 @@ __device__ __forceinline__ void mbar_init_fence() { asm volatile("fence.mbarrier
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Relaxed: it hands over tensor memory that has been read (ordered by the tcgen05 fence in front), no other memory.
+// With release it waited for every store under way to global memory.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // One thread of a warp whose threads are all here, always the same one.
 __device__ __forceinline__ bool elect_one() {
@@ -46,26 +48,19 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(chosen));
     return chosen != 0;
 }
-// CLUSTER: for arrivals of another CTA's threads (what TMA and the matrix unit signal needs no wider scope).
-template <bool CLUSTER>
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
-    if (CLUSTER)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
 // A whole warp waits for the phase; false, for all of its threads, when the limit passed for one of them or another
 // warp of the CTA gave up (*gave_up, in shared memory).
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint64_t limit_ns) {
-    bool done = mbar_try<CLUSTER>(bar, parity);
+    bool done = mbar_try(bar, parity);
     uint64_t t0 = 0;
     for (uint32_t polls = 1; !done && polls < kWaitLimitPolls; ++polls) {
-        done = mbar_try<CLUSTER>(bar, parity);
+        done = mbar_try(bar, parity);
         if (!done && (polls & 63u) == 0) {
             if (*gave_up) break;
             const uint64_t t = global_timer_ns();
@@ -77,10 +72,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (!done) *gave_up = 1;
     return done;
 }
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint64_t limit_ns) {
-    return mbar_wait<true>(bar, parity, gave_up, limit_ns);
-}
-
 // ---- TMA -----------------------------------------------------------------------------------------------------------
 
 // One box into this CTA's shared memory; the bytes are counted on a barrier of either CTA of the pair.
