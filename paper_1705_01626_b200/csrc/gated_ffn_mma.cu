@@ -1,7 +1,5 @@
 // Plan, workspace and dispatch of the gated feed-forward block on the matrix units; the kernels are in
 // gated_ffn_mma.cuh, instantiated for each type in a file of its own.
-#include <utility>
-
 #include "gated_ffn_mma.cuh"
 
 namespace cdma {
@@ -39,18 +37,12 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
 }
 
 uint32_t gate_cols(uint32_t tile_rows, uint32_t f) {
-    // The choice whose rounds over the pairs cost least.  A step of a narrow tile costs more for each column (it brings
-    // as many rows of x), so it pays only where wide tiles leave pairs idle.
-    uint32_t best = 256;
-    double least = 0;
-    for (const auto& [cols, cost] : {std::pair<uint32_t, double>{256, 1.0}, {128, 0.58}, {64, 0.36}}) {
-        const uint64_t items = static_cast<uint64_t>(tile_rows) * tiles_of(f, cols / 2);
-        const double t = cost * static_cast<double>((items + kPairs - 1) / kPairs);
-        if (least == 0 || t < least) { least = t; best = cols; }
-    }
-    return best;
+    // The choice whose rounds over the pairs cost less.  A step of 128 columns takes 350 cycles, one of 256 takes 515: the
+    // matrix unit is as long at fetching A for either (and for 64 columns).  Narrow tiles pay where wide ones leave pairs
+    // idle.
+    const auto rounds = [&](uint32_t cols) { return (static_cast<uint64_t>(tile_rows) * tiles_of(f, cols / 2) + kPairs - 1) / kPairs; };
+    return rounds(128) * 350 < rounds(256) * 515 ? 128 : 256;
 }
-
 extern template cudaError_t launch_all<float>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);
 extern template cudaError_t launch_all<__half>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);
 extern template cudaError_t launch_all<__nv_bfloat16>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);

@@ -680,10 +680,8 @@ cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix&
     if constexpr (sizeof(T) == 4) {
         return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
     } else {
-        const uint32_t cols = gate_cols(a.tile_rows, a.p.f);
-        if (cols == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
-        if (cols == 128) return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
-        return launch_gate_of<T, BACKWARD, 64>(maps, a, wg, wu, ctl, stream);
+        if (gate_cols(a.tile_rows, a.p.f) == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
+        return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
     }
 }
 

@@ -176,9 +176,11 @@ cudaError_t launch_type(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t 
     const uint32_t tiles = tiles_of(p.f, kTile);
     a.splits = 1;
     while (a.splits < 8 && tiles * a.splits * 2 <= 296 && a.steps / (a.splits * 2) >= 4) a.splits *= 2;
-    // one CTA to an SM may take all of its shared memory, else two share it
+    // One CTA to an SM may take all of its shared memory, else two share it -- not quite all of it: what waits in the
+    // memory system delays the next launch's first steps (1 x 4096 x 10944: five steps of 18 KB 33.2 us, four 34.1, six
+    // 36.9, twelve on an SM of its own 43.8).
     const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
-    const uint32_t room = tiles * a.splits <= 148 ? 220 * 1024 : 108 * 1024;
+    const uint32_t room = tiles * a.splits <= 148 ? 220 * 1024 : 96 * 1024;
     a.stages = room / stage_bytes < kMaxStages ? room / stage_bytes : kMaxStages;
     const uint32_t least = tiles_of(a.cols * kPitch * 4, stage_bytes);      // room for the turned accumulator
     const uint32_t most = tiles_of(a.steps, a.splits);
