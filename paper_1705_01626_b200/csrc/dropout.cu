@@ -3,6 +3,7 @@
 #include "chained_launch.cuh"
 #include "dropout.cuh"
 #include "elements.cuh"
+#include "fixed_divisor.cuh"
 #include "operand_checks.h"
 #include "zvc_common.cuh"
 
@@ -10,27 +11,6 @@ namespace cdma {
 namespace {
 
 constexpr uint32_t kThreads = 256;
-
-// Quotient of a 32-bit number and a fixed divisor by a high product (Granlund and Montgomery, "Division by
-// invariant integers using multiplication", PLDI 1994): a tensor's blocks are numbered through its rows, and a
-// division for each would cost as much as the generator.
-struct FixedDivisor {
-    uint32_t divisor, multiplier, shift1, shift2;
-};
-FixedDivisor make_divisor(uint32_t d) {
-    uint32_t l = 0;
-    while ((1ull << l) < d) ++l;
-    FixedDivisor f;
-    f.divisor = d;
-    f.multiplier = static_cast<uint32_t>((((1ull << l) - d) << 32) / d + 1);
-    f.shift1 = l < 1 ? l : 1;
-    f.shift2 = l < 1 ? 0 : l - 1;
-    return f;
-}
-__device__ __forceinline__ uint32_t divide(uint32_t n, const FixedDivisor& f) {
-    const uint32_t t = __umulhi(f.multiplier, n);
-    return (t + ((n - t) >> f.shift1)) >> f.shift2;
-}
 
 template <typename T> struct Args {
     const T* x;

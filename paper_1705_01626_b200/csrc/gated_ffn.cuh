@@ -86,10 +86,10 @@ __device__ __forceinline__ void gated_gradients(float g, float u, float dh, bool
     *dg = keep ? by_g : 0.0f;
 }
 
-// Forward pass of few rows: of 2-byte elements with strides that TMA takes (gated_ffn_stream.cu) ...
+// Few rows of 2-byte elements with strides that TMA takes (gated_ffn_stream.cu): h or, with `grads`, dG and dU ...
 constexpr uint64_t kFewRows = 128;
-cudaError_t launch_ffn_stream(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
-// ... and of 4-byte elements (gated_ffn_rows.cu).
+cudaError_t launch_ffn_stream(const FfnProblem& p, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream);
+// ... and of 4-byte elements, the forward pass alone (gated_ffn_rows.cu).
 constexpr uint64_t kFewRows4 = 8;
 cudaError_t launch_ffn_rows(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
 // Any number of rows (gated_ffn_mma.cu).

@@ -20,16 +20,27 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
     l.wu = l.wg + (needs_copy(ld_wg, f, dtype) ? round256(f * pitch_of(k) * copy) : 0);
     l.dx_partial = l.wu + (needs_copy(ld_wu, f, dtype) ? round256(f * pitch_of(k) * copy) : 0);
     l.dw_partial = l.end = l.dx_partial;
-    if (!backward) return l;
-    l.dx = Product{dx ? tiles_of(m, kTileRows) : 0, tiles_of(k, product_cols(dtype == CDMA_F32 ? 4 : 2)), tiles_of(f, kStep), static_cast<uint32_t>(2 * products), 1, nullptr, pitch_of(k), m};
-    l.dw = Product{dw ? 2 * tiles_of(f, kTileRows) : 0, tiles_of(k, product_cols(dtype == CDMA_F32 ? 4 : 2)), tiles_of(m, kStep), static_cast<uint32_t>(products), 1, nullptr, pitch_of(k), 2 * f};
+    if (!backward || m == 0 || k == 0 || f == 0) return l;      // nothing to multiply: no kernel follows
+    const uint32_t cols = tiles_of(k, product_cols(dtype == CDMA_F32 ? 4 : 2));
+    l.dx.tiles = make_tiles(dx ? tiles_of(m, kTileRows) : 0, cols);
+    l.dx.steps = tiles_of(f, kStep);
+    l.dx.parts = static_cast<uint32_t>(2 * products);
+    l.dx.rows_partial = m;
+    l.dw.tiles = make_tiles(dw ? 2 * tiles_of(f, kTileRows) : 0, cols);
+    l.dw.steps = tiles_of(m, kStep);
+    l.dw.parts = static_cast<uint32_t>(products);
+    l.dw.rows_partial = 2 * f;
     // an even share of all steps for each pair of SMs: longer tiles are cut to about that
     uint64_t all = 0;
-    for (const Product* q : {&l.dx, &l.dw}) all += static_cast<uint64_t>(q->tile_rows) * q->tile_cols * q->steps * q->parts;
+    for (const Product* q : {&l.dx, &l.dw}) all += static_cast<uint64_t>(q->tiles.rows) * q->tiles.cols * q->steps * q->parts;
     const uint64_t share = all / kPairs > kLeastSteps ? all / kPairs : kLeastSteps;
     for (Product* q : {&l.dx, &l.dw}) {
         const uint64_t steps = static_cast<uint64_t>(q->steps) * q->parts;
-        if (steps >= 2 * share) q->splits = static_cast<uint32_t>(steps / share < 32 ? steps / share : 32);
+        q->splits = steps < 2 * share ? 1 : static_cast<uint32_t>(steps / share < 32 ? steps / share : 32);
+        q->share = static_cast<uint32_t>(steps / q->splits);
+        q->longer = static_cast<uint32_t>(steps % q->splits);
+        q->by_steps = make_divisor(q->steps);
+        q->ld_partial = pitch_of(k);
     }
     l.dw_partial = l.dx_partial + (l.dx.splits > 1 && dx ? round256(l.dx.splits * l.dx.rows_partial * l.dx.ld_partial * 4) : 0);
     l.end = l.dw_partial + (l.dw.splits > 1 && dw ? round256(l.dw.splits * l.dw.rows_partial * l.dw.ld_partial * 4) : 0);

@@ -22,6 +22,7 @@
 #pragma once
 
 #include "chained_launch.cuh"
+#include "fixed_divisor.cuh"
 #include "gated_ffn.cuh"
 #include "gated_ffn_maps.cuh"
 #include "tcgen05.cuh"
@@ -73,15 +74,38 @@ struct Gradients {      // dG then dU, each in its planes: `m` rows of `ld` 2-by
     uint16_t* at;
     uint64_t ld;
 };
+// Output tiles of a product, in bands of kBand tile rows, down a band's column first: the tiles that run at one time
+// then share few rows of either operand, which stay in L2.  (Divisions by numbers that the host knows: each role of a
+// CTA goes through them for each tile, and tiles of a few steps waited for them.)
+struct Tiles {
+    uint32_t rows, cols;
+    FixedDivisor all, per_band, last_height;
+    __device__ __forceinline__ void place(uint32_t tile, uint32_t* row, uint32_t* col) const {
+        const uint32_t band = divide(tile, per_band), rest = tile - band * per_band.divisor;
+        const uint32_t c = (band + 1) * kBand <= rows ? rest / kBand : divide(rest, last_height);
+        const uint32_t height = (band + 1) * kBand <= rows ? kBand : last_height.divisor;
+        *row = band * kBand + rest - c * height;
+        *col = c;
+    }
+};
+inline Tiles make_tiles(uint32_t rows, uint32_t cols) {
+    const uint32_t r = rows != 0 ? rows : 1;
+    return Tiles{rows, cols, make_divisor(r * cols), make_divisor(kBand * cols), make_divisor(r % kBand != 0 ? r % kBand : kBand)};
+}
+
 struct GateArgs {
     FfnProblem p;
-    uint32_t tile_rows, tile_cols, steps;
+    Tiles tiles;
+    uint32_t steps;
     Gradients grads;
 };
 // Tiles of one product.  With splits > 1 each tile's reduction is cut into that many items, which leave sums in 32
 // bits for the joining kernel: where there are fewer tiles than pairs of SMs.
 struct Product {
-    uint32_t tile_rows, tile_cols, steps, parts, splits;
+    Tiles tiles;
+    FixedDivisor by_steps;
+    uint32_t steps, parts, splits;
+    uint32_t share, longer;      // steps of an item; the first `longer` splits have one more
     float* partial;
     uint64_t ld_partial, rows_partial;
 };
@@ -96,31 +120,22 @@ struct Item {
     uint32_t row, col;        // of the tile
     uint32_t first, last;     // steps, counted through the parts
     uint32_t steps, split;
+    uint32_t part;            // of the first step
     uint32_t small;           // steps of the small products of planes, which come first
 };
 
-// Tiles in bands of kBand tile rows, down a band's column first: the tiles that run at one time then share few rows
-// of either operand, which stay in L2.
-__device__ __forceinline__ void place(uint32_t tile, uint32_t tile_rows, uint32_t tile_cols, uint32_t* row, uint32_t* col) {
-    const uint32_t per_band = kBand * tile_cols;
-    const uint32_t band = tile / per_band, rest = tile % per_band;
-    const uint32_t height = min(kBand, tile_rows - band * kBand);
-    *row = band * kBand + rest % height;
-    *col = rest / height;
-}
-
 template <typename T>
-__device__ __forceinline__ uint32_t items_of(const GateArgs& a) { return a.tile_rows * a.tile_cols; }
+__device__ __forceinline__ uint32_t items_of(const GateArgs& a) { return a.tiles.rows * a.tiles.cols; }
 template <typename T>
 __device__ __forceinline__ Item item_of(const GateArgs& a, uint32_t index) {
     Item it{};
-    place(index, a.tile_rows, a.tile_cols, &it.row, &it.col);
+    a.tiles.place(index, &it.row, &it.col);
     it.steps = a.steps;
     it.last = a.steps * Planes<T>::products;
     it.small = it.last - a.steps;
     return it;
 }
-__device__ __forceinline__ uint32_t items_of(const Product& q) { return q.tile_rows * q.tile_cols * q.splits; }
+__host__ __device__ __forceinline__ uint32_t items_of(const Product& q) { return q.tiles.rows * q.tiles.cols * q.splits; }
 template <typename T>
 __device__ __forceinline__ uint32_t items_of(const ProductsArgs& a) { return items_of(a.dx) + items_of(a.dw); }
 template <typename T>
@@ -128,17 +143,17 @@ __device__ __forceinline__ Item item_of(const ProductsArgs& a, uint32_t index) {
     Item it{};
     it.dw = index >= items_of(a.dx);
     const Product& q = it.dw ? a.dw : a.dx;
-    const uint32_t i = it.dw ? index - items_of(a.dx) : index, tiles = q.tile_rows * q.tile_cols;
-    it.split = i / tiles;
-    place(i % tiles, q.tile_rows, q.tile_cols, &it.row, &it.col);
-    const uint64_t total = static_cast<uint64_t>(q.steps) * q.parts;
-    it.first = static_cast<uint32_t>(total * it.split / q.splits);
-    it.last = static_cast<uint32_t>(total * (it.split + 1) / q.splits);
+    const uint32_t i = it.dw ? index - items_of(a.dx) : index;
+    it.split = divide(i, q.tiles.all);
+    q.tiles.place(i - it.split * q.tiles.all.divisor, &it.row, &it.col);
+    it.first = it.split * q.share + min(it.split, q.longer);
+    it.last = it.first + q.share + (it.split < q.longer ? 1 : 0);
     it.steps = q.steps;
-    it.small = static_cast<uint32_t>(total) - (it.dw ? 1 : 2) * q.steps;
-    if (it.dw && it.row >= q.tile_rows / 2) {      // the upper half of the tile rows are dWu's
+    it.small = q.steps * q.parts - (it.dw ? 1 : 2) * q.steps;
+    it.part = divide(it.first, q.by_steps);
+    if (it.dw && it.row >= q.tiles.rows / 2) {      // the upper half of the tile rows are dWu's
         it.second = true;
-        it.row -= q.tile_rows / 2;
+        it.row -= q.tiles.rows / 2;
     }
     return it;
 }
@@ -233,11 +248,34 @@ __device__ __forceinline__ void store_planes8(uint16_t* to, uint64_t plane, cons
     for (int j = 0; j < 3; ++j) *reinterpret_cast<uint4*>(to + j * plane) = make_uint4(words[j][0], words[j][1], words[j][2], words[j][3]);
 }
 
-// 32 hidden columns of the warp's 32 rows: h, or dG and dU; G at tensor-memory place `g`, U at `u`.  Eight columns at
+// The thread's row of a 32 x 32 block of dh in registers (2-byte elements), fetched while the accumulator is still
+// collected.
+template <typename T>
+__device__ __forceinline__ void fetch_dh(uint8_t* turn, uint32_t (&words)[16], const T* at, uint64_t ld, int64_t rows, int64_t cols) {
+    const uint4* from;
+    bool there = true;
+    if (cols >= 32 && ((reinterpret_cast<uintptr_t>(at) | ld * sizeof(T)) & 15u) == 0) {
+        from = reinterpret_cast<const uint4*>(at + lane_id() * ld);
+        there = lane_id() < rows;
+    } else {
+        move_block<T, false>(turn, const_cast<T*>(at), ld, rows, cols);
+        from = reinterpret_cast<const uint4*>(turn + lane_id() * kTurnPitch<T>);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 v = there ? from[i] : make_uint4(0, 0, 0, 0);
+        words[4 * i] = v.x; words[4 * i + 1] = v.y; words[4 * i + 2] = v.z; words[4 * i + 3] = v.w;
+    }
+    __syncwarp();
+}
+
+// 32 hidden columns of the warp's 32 rows: h, or dG and dU; G at tensor-memory place `g`, U at `u`.  dh: in `words`, or
+// in the turning block for 4-byte elements.  Eight columns at
 // a time in a rolled loop: unrolled over all columns the code does not fit the instruction cache, and the first tile
 // of a launch, often its only one, waited for instructions most of the time (GELU: 37,000 cycles for 32 columns).
 template <typename T, int ACT, bool BACKWARD>
-__device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, uint32_t row, uint32_t col, uint32_t g, uint32_t u) {
+__device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, uint32_t row, uint32_t col, uint32_t g, uint32_t u,
+                                            uint32_t (&words)[16]) {
     const FfnProblem& p = a.p;
     constexpr bool kFast = sizeof(T) == 2;
     uint8_t* second = turn + 32 * kTurnPitch<T>;
@@ -251,7 +289,18 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
     for (uint32_t c = 0; c < 32; c += 8) {
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row + lane_id(), (col + c) >> 3) : 0xffu;
         float dh[8], first[8], other[8];
-        if (BACKWARD) get8<T>(turn, c, dh);
+        if constexpr (BACKWARD && sizeof(T) == 4) {
+            get8<T>(turn, c, dh);
+        } else if constexpr (BACKWARD) {      // the next eight move to the front: a rolled loop cannot pick registers
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = unpack2<T>(words[i]);
+                dh[2 * i] = v.x;
+                dh[2 * i + 1] = v.y;
+            }
+#pragma unroll
+            for (int i = 0; i < 12; ++i) words[i] = words[i + 4];
+        }
         uint32_t gw[8], uw[8];
         tmem_load_wait();
 #pragma unroll
@@ -321,7 +370,7 @@ __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map
         const Item it = item_of<T>(a, index);
         const uint32_t row = it.row * kTileRows + rank * 128;
         const uint32_t col = C::kGate ? it.col * (C::kCols / 2) : it.col * C::kCols + rank * (C::kCols / 2);
-        uint32_t part = it.first / it.steps, r = it.first % it.steps * kStep;
+        uint32_t part = it.part, r = (it.first - it.part * it.steps) * kStep;
         for (uint32_t s = it.first; s < it.last; ++s) {
             if (!(fine = mbar_wait(empty + 8 * ring.stage, ring.phase ^ 1u, &c.gave_up, ctl.wait_limit_ns))) break;
             const uint32_t bar = full + 8 * ring.stage;
@@ -426,13 +475,20 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
     for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
         const Item it = item_of<T>(a, index);
         const uint32_t row = it.row * kTileRows + rank * 128 + quarter * 32;      // the warp's first
-        auto load_dh = [&](uint32_t i) {
-            const uint32_t col = it.col * (C::kCols / 2) + i * 32;
-            if (row < p.m && col < p.f)
-                move_block<T, false>(turn, const_cast<T*>(static_cast<const T*>(p.dh)) + row * p.ld_h + col, p.ld_h,
-                                     static_cast<int64_t>(p.m) - row, static_cast<int64_t>(p.f) - col);
-        };
-        if (C::kBackward && half < kBlocks) load_dh(half);      // while the accumulator is still collected
+        // dh of the warp's blocks, while the accumulator is still collected
+        constexpr uint32_t kOwn = C::kGate ? (kBlocks + 1) / 2 : 1;
+        uint32_t words[kOwn][16];
+        if constexpr (C::kGate && C::kBackward) {
+#pragma unroll
+            for (uint32_t i = 0; i < kOwn; ++i) {
+                const uint32_t col = it.col * (C::kCols / 2) + (half + 2 * i) * 32;
+                if (row >= p.m || col >= p.f) continue;
+                const T* at = static_cast<const T*>(p.dh) + row * p.ld_h + col;
+                const int64_t rows = static_cast<int64_t>(p.m) - row, cols = static_cast<int64_t>(p.f) - col;
+                if constexpr (sizeof(T) == 2) fetch_dh<T>(turn, words[i], at, p.ld_h, rows, cols);
+                else move_block<T, false>(turn, const_cast<T*>(at), p.ld_h, rows, cols);
+            }
+        }
         uint32_t from = tmem;
         for (uint32_t s = it.first; s < it.last; ++n) {
             const uint32_t end = end_of_stretch<T>(it, s), acc = n & 1u;
@@ -462,10 +518,14 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
         if (!fine) break;
         if constexpr (sizeof(T) == 4) from = sums;
         if constexpr (C::kGate) {
+            static_assert(sizeof(T) == 2 || kOwn == 1, "one turning block holds one block of dh");
 #pragma unroll 1
             for (uint32_t i = half; i < kBlocks; i += 2) {
-                if (C::kBackward && i != half) load_dh(i);
-                finish_gate<T, ACT, C::kBackward>(a, turn, row, it.col * (C::kCols / 2) + i * 32, from + i * 32, from + C::kCols / 2 + i * 32);
+                finish_gate<T, ACT, C::kBackward>(a, turn, row, it.col * (C::kCols / 2) + i * 32, from + i * 32, from + C::kCols / 2 + i * 32, words[0]);
+                if constexpr (C::kBackward && kOwn == 2) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) words[0][j] = words[1][j];
+                }
             }
         } else {
             const Product& q = it.dw ? a.dw : a.dx;
@@ -668,9 +728,9 @@ cudaError_t launch_kernel(const CUtensorMap (&maps)[4], const Args& a, uint64_t 
 template <typename T, bool BACKWARD, uint32_t COLS>
 cudaError_t launch_gate_of(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
     using C = Config<true, BACKWARD, COLS, T>;
-    a.tile_cols = tiles_of(a.p.f, COLS / 2);
+    a.tiles = make_tiles(a.tiles.rows, tiles_of(a.p.f, COLS / 2));
     if (!make_operand_map(&maps[2], wg, a.p.dtype, COLS / 2) || !make_operand_map(&maps[3], wu, a.p.dtype, COLS / 2)) return cudaErrorInvalidValue;
-    const uint64_t items = static_cast<uint64_t>(a.tile_rows) * a.tile_cols;
+    const uint64_t items = static_cast<uint64_t>(a.tiles.rows) * a.tiles.cols;
     if (a.p.activation == CDMA_ACT_RELU) return launch_kernel<C, T, CDMA_ACT_RELU>(maps, a, items, ctl, stream);
     if (a.p.activation == CDMA_ACT_SILU) return launch_kernel<C, T, CDMA_ACT_SILU>(maps, a, items, ctl, stream);
     return launch_kernel<C, T, CDMA_ACT_GELU>(maps, a, items, ctl, stream);
@@ -680,7 +740,7 @@ cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix&
     if constexpr (sizeof(T) == 4) {
         return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
     } else {
-        if (gate_cols(a.tile_rows, a.p.f) == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
+        if (gate_cols(a.tiles.rows, a.p.f) == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
         return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
     }
 }
@@ -726,20 +786,20 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     cudaError_t e = prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
     if (e != cudaSuccess) return e;
     const Matrix &x = operands[0], &wg = operands[1], &wu = operands[2];
-    if (!backward && p.dtype != CDMA_F32 && p.m <= kFewRows) {
-        FfnProblem few = p;
-        few.x = x.p, few.wg = wg.p, few.wu = wu.p;
-        few.ld_x = x.ld, few.ld_wg = wg.ld, few.ld_wu = wu.ld;
-        return launch_ffn_stream(few, ctl, stream);
-    }
-
     CUtensorMap maps[4];
     const uint64_t pitch = pitch_of(p.f);
     const Matrix grads{ws + l.grads, p.m, p.f, pitch, 2 * planes_of(p.dtype)};
-    GateArgs g{p, tiles_of(p.m, kTileRows), 0, tiles_of(p.k, kStep), {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
+    GateArgs g{p, make_tiles(tiles_of(p.m, kTileRows), 1), tiles_of(p.k, kStep), {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
     if (!make_operand_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
     maps[1] = maps[0];
-    e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
+    if (sizeof(T) == 2 && p.m <= kFewRows) {
+        FfnProblem few = p;
+        few.x = x.p, few.wg = wg.p, few.wu = wu.p;
+        few.ld_x = x.ld, few.ld_wg = wg.ld, few.ld_wu = wu.ld;
+        e = launch_ffn_stream(few, backward ? ws + l.grads : nullptr, pitch, ctl, stream);
+    } else {
+        e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
+    }
     if (e != cudaSuccess || !backward) return e;
 
     ProductsArgs a{p, l.dx, l.dw};
@@ -748,8 +808,7 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     if (!make_operand_map(&maps[0], x, p.dtype, kStep) || !make_operand_map(&maps[1], grads, p.dtype, kStep) || !make_operand_map(&maps[2], wg, p.dtype, kStep) ||
         !make_operand_map(&maps[3], wu, p.dtype, kStep))
         return cudaErrorInvalidValue;
-    const uint64_t items = static_cast<uint64_t>(a.dx.tile_rows) * a.dx.tile_cols * a.dx.splits +
-                           static_cast<uint64_t>(a.dw.tile_rows) * a.dw.tile_cols * a.dw.splits;
+    const uint64_t items = static_cast<uint64_t>(items_of(a.dx)) + items_of(a.dw);
     e = launch_kernel<Config<false, false, product_cols(sizeof(T)), T>, T, 0>(maps, a, items, ctl, stream);
     if (e == cudaSuccess && p.dx != nullptr && a.dx.splits > 1) e = join<T>(a.dx, p.dx, nullptr, p.ld_dx, p.m, p.k, stream);
     if (e == cudaSuccess && p.dwg != nullptr && a.dw.splits > 1) e = join<T>(a.dw, p.dwg, p.dwu, p.ld_dw, p.f, p.k, stream);

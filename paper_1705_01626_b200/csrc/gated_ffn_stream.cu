@@ -1,5 +1,5 @@
-// Forward pass of the gated feed-forward block for few rows of 2-byte elements (a decoding step, a short prompt):
-// bound by the bytes of the weights, so the kernel is a stream of the weights through shared memory into the matrix
+// G and U of the gated feed-forward block for few rows of 2-byte elements (a decoding step, a short prompt), and from
+// them h or, in the backward pass, dG and dU: bound by the bytes of the weights, so the kernel is a stream of the weights through shared memory into the matrix
 // units, each element read once.
 //
 // The weights are operand A: 64 rows of Wg and the same 64 of Wu are the 128 rows of a tile, the rows of x, rounded
@@ -34,6 +34,8 @@ struct __align__(8) Control {
 struct StreamArgs {
     FfnProblem p;
     uint32_t steps, splits, cols, columns, stages;     // cols: rows of x, rounded up; columns: of tensor memory
+    void* grads;                                       // backward: dG, then dU, m rows of ld_grad
+    uint64_t ld_grad;
 };
 
 __device__ __forceinline__ float load_from_cta(uint32_t address, uint32_t rank) {
@@ -42,7 +44,7 @@ __device__ __forceinline__ float load_from_cta(uint32_t address, uint32_t rank) 
     return v;
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, bool BACKWARD>
 __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
                                                               const __grid_constant__ CUtensorMap map_wu,
                                                               const __grid_constant__ StreamArgs a, const LaunchCtl ctl) {
@@ -149,7 +151,15 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             }
         }
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row, (f0 + j) >> 3) >> (j & 7u) : 1u;
-        static_cast<T*>(p.h)[row * p.ld_h + f0 + j] = from_float<T>(gated_value<ACT, true>(g, u, keep & 1u, p.drop.scale));
+        if (BACKWARD) {
+            float dg, du;
+            gated_gradients<ACT, true>(g, u, to_float(static_cast<const T*>(p.dh)[row * p.ld_h + f0 + j]), keep & 1u, p.drop.scale, &dg, &du);
+            T* to = static_cast<T*>(a.grads) + row * a.ld_grad + f0 + j;
+            to[0] = from_float<T>(dg);
+            to[p.m * a.ld_grad] = from_float<T>(du);
+        } else {
+            static_cast<T*>(p.h)[row * p.ld_h + f0 + j] = from_float<T>(gated_value<ACT, true>(g, u, keep & 1u, p.drop.scale));
+        }
     }
     __syncthreads();
     if (a.splits > 1) cluster_sync();      // nobody leaves while its sums are read
@@ -158,16 +168,18 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
 
 template <typename T, int ACT>
 cudaError_t launch_kernel(const CUtensorMap (&maps)[3], const StreamArgs& a, uint32_t tiles, uint32_t smem, const LaunchCtl& ctl, cudaStream_t stream) {
-    auto kernel = ffn_stream_kernel<T, ACT>;
+    auto kernel = a.grads != nullptr ? ffn_stream_kernel<T, ACT, true> : ffn_stream_kernel<T, ACT, false>;
     const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), 232448 - sizeof(Control) - 64);
     if (e != cudaSuccess) return e;
     return launch_chained(kernel, tiles * a.splits, kThreads, smem, a.splits, stream, maps[0], maps[1], maps[2], a, ctl);
 }
 
 template <typename T>
-cudaError_t launch_type(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
+cudaError_t launch_type(const FfnProblem& p, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream) {
     StreamArgs a{};
     a.p = p;
+    a.grads = grads;
+    a.ld_grad = ld_grad;
     a.steps = tiles_of(p.k, kStep);
     a.cols = (p.m + 15) & ~15u;
     a.columns = 32;
@@ -199,8 +211,9 @@ cudaError_t launch_type(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t 
 
 }  // namespace
 
-cudaError_t launch_ffn_stream(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream) {
-    return p.dtype == CDMA_F16 ? launch_type<__half>(p, ctl, stream) : launch_type<__nv_bfloat16>(p, ctl, stream);
+cudaError_t launch_ffn_stream(const FfnProblem& p, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream) {
+    return p.dtype == CDMA_F16 ? launch_type<__half>(p, grads, ld_grad, ctl, stream)
+                               : launch_type<__nv_bfloat16>(p, grads, ld_grad, ctl, stream);
 }
 
 }  // namespace cdma

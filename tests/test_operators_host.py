@@ -92,3 +92,10 @@ def test_gated_ffn_workspace():
             fwd, bwd = B.cdma_gated_ffn_workspace_bytes(d, 0), B.cdma_gated_ffn_workspace_bytes(d, 1)
             assert fwd >= 256 and fwd % 256 == 0 and bwd % 256 == 0
             assert bwd >= 2 * m * f * s             # the gradients of G and U
+
+
+def test_gated_ffn_workspace_of_empty_blocks():
+    for m, k, f in ((0, 8, 16), (4, 0, 16), (4, 8, 0), (0, 0, 0)):
+        for dtype in (B.F32, B.F16):
+            for backward in (0, 1):
+                assert B.cdma_gated_ffn_workspace_bytes(desc(m=m, k=k, f=f, dtype=dtype), backward) >= 256
