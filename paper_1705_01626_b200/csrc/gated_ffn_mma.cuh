@@ -189,6 +189,12 @@ __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, in
     __syncwarp();
 }
 
+// 32 bytes of one thread: a whole sector, so that rows can be stored from registers without turning.
+__device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
 // The three bf16 planes of a float, cut off so that the two upper ones never round up to infinity.  What is not
 // finite goes into the first plane alone.
 __device__ __forceinline__ void split3(float v, uint32_t (&planes)[3]) {
@@ -543,11 +549,29 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
                 for (int j = 0; j < 32; ++j) v[j] = next[j];
                 if (i + 2 < kBlocks) tmem_load32(from + (i + 2) * 32, next);
                 if (row >= rows || col >= p.k) continue;
+                const int64_t rows_left = static_cast<int64_t>(rows) - row, cols_left = static_cast<int64_t>(p.k) - col;
+                T* to = out + row * ld + col;
                 if (q.splits > 1) {
-                    if (row + lane < rows) {
-                        float* to = q.partial + (it.split * q.rows_partial + (it.second ? rows : 0) + row + lane) * q.ld_partial + col;
+                    if (lane < rows_left) {
+                        float* sum = q.partial + (it.split * q.rows_partial + (it.second ? rows : 0) + row + lane) * q.ld_partial + col;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) reinterpret_cast<uint4*>(to)[j] = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                        for (int j = 0; j < 32; j += 8) {
+                            const uint32_t w[8] = {v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]};
+                            store32(sum + j, w);
+                        }
+                    }
+                } else if (cols_left >= 32 && ((reinterpret_cast<uintptr_t>(out) | ld * sizeof(T)) & 31u) == 0) {
+                    if (lane < rows_left) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 32 / sizeof(T)) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if constexpr (sizeof(T) == 4) w[i] = v[j + i];
+                                else w[i] = pack2<T>(__uint_as_float(v[j + 2 * i]), __uint_as_float(v[j + 2 * i + 1]));
+                            }
+                            store32(to + lane * ld + j, w);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -556,7 +580,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
                                                 __uint_as_float(v[j + 4]), __uint_as_float(v[j + 5]), __uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])};
                         put8<T>(turn, j, eight);
                     }
-                    move_block<T, true>(turn, out + row * ld + col, ld, static_cast<int64_t>(rows) - row, static_cast<int64_t>(p.k) - col);
+                    move_block<T, true>(turn, to, ld, rows_left, cols_left);
                 }
             }
         }
