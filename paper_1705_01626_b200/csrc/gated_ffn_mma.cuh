@@ -34,8 +34,6 @@ constexpr uint32_t kPairs = 74;                      // pairs of SMs
 constexpr uint32_t kStep = 64;                       // reduction elements per step: 128 bytes
 constexpr uint32_t kHalfBytes = 128 * kStep * 2;     // one CTA's half of A: 128 rows
 constexpr uint32_t kTileRows = 256;
-constexpr uint32_t kReaderWarps = 8;
-constexpr uint32_t kThreads = 32 * (4 + kReaderWarps);
 constexpr uint32_t kBand = 16;                       // tile rows that are walked together
 constexpr uint32_t kMaxStages = 9;
 
@@ -45,26 +43,33 @@ template <> struct Planes<float> { static constexpr uint32_t count = 3, products
 constexpr uint32_t kPlaneOfA = 0x010120u, kPlaneOfB = 0x001102u;
 
 // Warp-private block of shared memory through which 32 x 32 elements turn: a thread has a row of them in registers,
-// memory wants neighbouring threads on neighbouring columns.  Rows are padded by 16 bytes: no bank conflicts.
-template <typename T> constexpr uint32_t kTurnPitch = 32 * sizeof(T) + 16;
+// memory wants neighbouring threads on neighbouring columns.  The 16-byte pieces of a row are swapped by the row's number
+// so that neither side meets a bank conflict.
+template <typename T> constexpr uint32_t kTurnBytes = 32 * 32 * sizeof(T);
+template <typename T>
+__device__ __forceinline__ uint8_t* turn_at(uint8_t* turn, uint32_t row, uint32_t piece) {
+    return turn + row * 32 * sizeof(T) + 16 * (sizeof(T) == 4 ? piece ^ (row & 7u) : piece ^ ((row >> 1) & 3u));
+}
 
 struct __align__(8) Control {
     uint64_t full[kMaxStages], empty[kMaxStages], done[2], free_[2];
     uint32_t tmem, gave_up;
 };
 
-// A kernel's shape: GATE or products, columns of a tile, and what follows from the type.
-template <bool GATE, bool BACKWARD, uint32_t COLS, typename T>
+// A kernel's shape: GATE or products, columns of a tile, warps that read the accumulators, and what follows from the type.
+template <bool GATE, bool BACKWARD, uint32_t COLS, uint32_t READERS, typename T>
 struct Config {
     static constexpr bool kGate = GATE, kBackward = BACKWARD;
     static constexpr uint32_t kCols = COLS;
     static constexpr uint32_t kStageBytes = kHalfBytes + COLS / 2 * kStep * 2;
+    static constexpr uint32_t kReaders = READERS;
+    static constexpr uint32_t kGroups = kReaders / 4, kThreads = 32 * (4 + kReaders);
     static constexpr uint32_t kTurnBlocks = GATE && BACKWARD && sizeof(T) == 2 ? 2 : 1;     // dG and dU are turned side by side
-    static constexpr uint32_t kTurnBytes = kReaderWarps * kTurnBlocks * 32 * kTurnPitch<T>;
+    static constexpr uint32_t kTurns = kReaders * kTurnBlocks * kTurnBytes<T>;
     // as many steps as fit beside the turning blocks and the barriers (227 KB)
-    static constexpr uint32_t kFit = (232448 - 1024 - sizeof(Control) - kTurnBytes) / kStageBytes;
+    static constexpr uint32_t kFit = (232448 - 1024 - sizeof(Control) - kTurns) / kStageBytes;
     static constexpr uint32_t kStages = kFit < kMaxStages ? kFit : kMaxStages;
-    static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + kTurnBytes + sizeof(Control);
+    static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + kTurns + sizeof(Control);
     // two accumulators; 4-byte elements have their running sums beside them
     static constexpr uint32_t kTmemCols = sizeof(T) == 4 ? 4 * COLS : 2 * COLS;
     static_assert(kTmemCols <= 512, "tensor memory has 512 columns");
@@ -164,7 +169,7 @@ __device__ __forceinline__ Item item_of(const ProductsArgs& a, uint32_t index) {
 // `at` + `ld` decide between 16-byte accesses and single elements; what does not exist is read as zero.
 template <typename T, bool STORE>
 __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, int64_t rows, int64_t cols) {
-    constexpr uint32_t kPitch = kTurnPitch<T>, kVectors = 32 * sizeof(T) / 16, kRowsAtOnce = 32 / kVectors;
+    constexpr uint32_t kPer = 16 / sizeof(T), kVectors = 32 / kPer, kRowsAtOnce = 32 / kVectors;
     const uint32_t lane = lane_id();
     __syncwarp();
     if (cols >= 32 && ((reinterpret_cast<uintptr_t>(at) | ld * sizeof(T)) & 15u) == 0) {
@@ -172,15 +177,15 @@ __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, in
 #pragma unroll
         for (uint32_t i = 0; i < kVectors; ++i) {
             const uint32_t r = i * kRowsAtOnce + first;
-            uint4* there = reinterpret_cast<uint4*>(at + r * ld + vector * (16 / sizeof(T)));
-            uint4* here = reinterpret_cast<uint4*>(turn + r * kPitch + 16 * vector);
+            uint4* there = reinterpret_cast<uint4*>(at + r * ld + vector * kPer);
+            uint4* here = reinterpret_cast<uint4*>(turn_at<T>(turn, r, vector));
             if (STORE) { if (r < rows) *there = *here; }
             else *here = r < rows ? __ldg(there) : make_uint4(0, 0, 0, 0);
         }
     } else {
 #pragma unroll 8
         for (uint32_t r = 0; r < 32; ++r) {
-            T* here = reinterpret_cast<T*>(turn + r * kPitch + lane * sizeof(T));
+            T* here = reinterpret_cast<T*>(turn_at<T>(turn, r, lane / kPer)) + lane % kPer;
             const bool exists = r < rows && lane < cols;
             if (STORE) { if (exists) at[r * ld + lane] = *here; }
             else *here = exists ? at[r * ld + lane] : from_float<T>(0.0f);
@@ -211,31 +216,19 @@ __device__ __forceinline__ void split3(float v, uint32_t (&planes)[3]) {
 // Eight neighbouring elements of the thread's row of the turning block.
 template <typename T>
 __device__ __forceinline__ void put8(uint8_t* turn, uint32_t col, const float (&v)[8]) {
-    uint4* to = reinterpret_cast<uint4*>(turn + lane_id() * kTurnPitch<T> + col * sizeof(T));
+    const auto piece = [&](uint32_t i) { return reinterpret_cast<uint4*>(turn_at<T>(turn, lane_id(), i)); };
     if constexpr (sizeof(T) == 4) {
-        to[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        to[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        *piece(col / 4) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        *piece(col / 4 + 1) = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
     } else {
-        to[0] = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+        *piece(col / 8) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
     }
 }
-template <typename T>
-__device__ __forceinline__ void get8(const uint8_t* turn, uint32_t col, float (&v)[8]) {
-    const uint4* from = reinterpret_cast<const uint4*>(turn + lane_id() * kTurnPitch<T> + col * sizeof(T));
-    const uint4 q = from[0];
-    if constexpr (sizeof(T) == 4) {
-        const uint4 r = from[1];
-        const uint32_t w[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+__device__ __forceinline__ void get8(uint8_t* turn, uint32_t col, float (&v)[8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    } else {
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = unpack2<T>(w[i]);
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
-        }
+    for (uint32_t i = 0; i < 2; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(turn_at<float>(turn, lane_id(), col / 4 + i));
+        v[4 * i] = q.x; v[4 * i + 1] = q.y; v[4 * i + 2] = q.z; v[4 * i + 3] = q.w;
     }
 }
 
@@ -258,18 +251,13 @@ __device__ __forceinline__ void store_planes8(uint16_t* to, uint64_t plane, cons
 // collected.
 template <typename T>
 __device__ __forceinline__ void fetch_dh(uint8_t* turn, uint32_t (&words)[16], const T* at, uint64_t ld, int64_t rows, int64_t cols) {
-    const uint4* from;
-    bool there = true;
-    if (cols >= 32 && ((reinterpret_cast<uintptr_t>(at) | ld * sizeof(T)) & 15u) == 0) {
-        from = reinterpret_cast<const uint4*>(at + lane_id() * ld);
-        there = lane_id() < rows;
-    } else {
-        move_block<T, false>(turn, const_cast<T*>(at), ld, rows, cols);
-        from = reinterpret_cast<const uint4*>(turn + lane_id() * kTurnPitch<T>);
-    }
+    const bool vectors = cols >= 32 && ((reinterpret_cast<uintptr_t>(at) | ld * sizeof(T)) & 15u) == 0;
+    if (!vectors) move_block<T, false>(turn, const_cast<T*>(at), ld, rows, cols);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint4 v = there ? from[i] : make_uint4(0, 0, 0, 0);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (!vectors) v = *reinterpret_cast<const uint4*>(turn_at<T>(turn, lane_id(), i));
+        else if (lane_id() < rows) v = __ldg(reinterpret_cast<const uint4*>(at + lane_id() * ld) + i);
         words[4 * i] = v.x; words[4 * i + 1] = v.y; words[4 * i + 2] = v.z; words[4 * i + 3] = v.w;
     }
     __syncwarp();
@@ -284,7 +272,7 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
                                             uint32_t (&words)[16]) {
     const FfnProblem& p = a.p;
     constexpr bool kFast = sizeof(T) == 2;
-    uint8_t* second = turn + 32 * kTurnPitch<T>;
+    uint8_t* second = turn + kTurnBytes<T>;
     const int64_t rows = static_cast<int64_t>(p.m) - row;
     uint16_t* grads = a.grads.at + (row + lane_id()) * a.grads.ld + col;
     const uint64_t plane = static_cast<uint64_t>(p.m) * a.grads.ld;
@@ -296,7 +284,7 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row + lane_id(), (col + c) >> 3) : 0xffu;
         float dh[8], first[8], other[8];
         if constexpr (BACKWARD && sizeof(T) == 4) {
-            get8<T>(turn, c, dh);
+            get8(turn, c, dh);
         } else if constexpr (BACKWARD) {      // the next eight move to the front: a rolled loop cannot pick registers
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -467,11 +455,11 @@ __device__ __forceinline__ void run_issuer(const Args& a, uint32_t base, Control
     }
 }
 
-// Eight warps: quarters of the accumulator's rows, every other block of 32 columns.
+// Reading warps: four take the quarters of the accumulator's rows, each group of four its blocks of 32 columns.
 template <typename C, typename T, int ACT, typename Args>
 __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Control& c, const LaunchCtl& ctl) {
-    const uint32_t warp = (threadIdx.x >> 5) - 4, quarter = warp & 3u, half = warp >> 2, rank = cluster_rank(), lane = lane_id();
-    uint8_t* turn = turns + warp * C::kTurnBlocks * 32 * kTurnPitch<T>;
+    const uint32_t warp = (threadIdx.x >> 5) - 4, quarter = warp & 3u, group = warp >> 2, rank = cluster_rank(), lane = lane_id();
+    uint8_t* turn = turns + warp * C::kTurnBlocks * kTurnBytes<T>;
     const uint32_t items = items_of<T>(a), free0 = in_cta(shared_address(&c.free_[0]), 0);
     const FfnProblem& p = a.p;
     const uint32_t tmem = c.tmem + (quarter * 32u << 16), sums = tmem + 2 * C::kCols;
@@ -482,12 +470,13 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
         const Item it = item_of<T>(a, index);
         const uint32_t row = it.row * kTileRows + rank * 128 + quarter * 32;      // the warp's first
         // dh of the warp's blocks, while the accumulator is still collected
-        constexpr uint32_t kOwn = C::kGate ? (kBlocks + 1) / 2 : 1;
+        constexpr uint32_t kOwn = C::kGate ? kBlocks / C::kGroups : 1;
+        static_assert(sizeof(T) == 2 || kOwn == 1, "the turning block holds one block of dh");
         uint32_t words[kOwn][16];
         if constexpr (C::kGate && C::kBackward) {
 #pragma unroll
             for (uint32_t i = 0; i < kOwn; ++i) {
-                const uint32_t col = it.col * (C::kCols / 2) + (half + 2 * i) * 32;
+                const uint32_t col = it.col * (C::kCols / 2) + (group + C::kGroups * i) * 32;
                 if (row >= p.m || col >= p.f) continue;
                 const T* at = static_cast<const T*>(p.dh) + row * p.ld_h + col;
                 const int64_t rows = static_cast<int64_t>(p.m) - row, cols = static_cast<int64_t>(p.f) - col;
@@ -504,7 +493,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             from = tmem + acc * C::kCols;
             if constexpr (sizeof(T) == 4) {
 #pragma unroll 1
-                for (uint32_t i = half; i < C::kCols / 32; i += 2) {
+                for (uint32_t i = group; i < C::kCols / 32; i += C::kGroups) {
                     // blocks of G and of U alternate between the warps as the gate's reader takes them
                     const uint32_t at = i * 32;
                     uint32_t v[32], w[32];
@@ -524,14 +513,10 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
         if (!fine) break;
         if constexpr (sizeof(T) == 4) from = sums;
         if constexpr (C::kGate) {
-            static_assert(sizeof(T) == 2 || kOwn == 1, "one turning block holds one block of dh");
-#pragma unroll 1
-            for (uint32_t i = half; i < kBlocks; i += 2) {
-                finish_gate<T, ACT, C::kBackward>(a, turn, row, it.col * (C::kCols / 2) + i * 32, from + i * 32, from + C::kCols / 2 + i * 32, words[0]);
-                if constexpr (C::kBackward && kOwn == 2) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) words[0][j] = words[1][j];
-                }
+            for (uint32_t i = 0; i < kOwn; ++i) {
+                const uint32_t block = (group + C::kGroups * i) * 32;
+                finish_gate<T, ACT, C::kBackward>(a, turn, row, it.col * (C::kCols / 2) + block, from + block, from + C::kCols / 2 + block, words[i]);
             }
         } else {
             const Product& q = it.dw ? a.dw : a.dx;
@@ -539,15 +524,15 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             const uint64_t ld = it.dw ? p.ld_dw : p.ld_dx;
             const uint32_t rows = it.dw ? p.f : p.m;
             uint32_t next[32];
-            tmem_load32(from + half * 32, next);
+            tmem_load32(from + group * 32, next);
 #pragma unroll 1
-            for (uint32_t i = half; i < kBlocks; i += 2) {
+            for (uint32_t i = group; i < kBlocks; i += C::kGroups) {
                 const uint32_t col = it.col * C::kCols + i * 32;
                 uint32_t v[32];
                 tmem_load_wait();
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = next[j];
-                if (i + 2 < kBlocks) tmem_load32(from + (i + 2) * 32, next);
+                if (i + C::kGroups < kBlocks) tmem_load32(from + (i + C::kGroups) * 32, next);
                 if (row >= rows || col >= p.k) continue;
                 const int64_t rows_left = static_cast<int64_t>(rows) - row, cols_left = static_cast<int64_t>(p.k) - col;
                 T* to = out + row * ld + col;
@@ -593,14 +578,14 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
 }
 
 template <typename C, typename T, int ACT, typename Args>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(C::kThreads, 1)
 ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g,
                const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
                const __grid_constant__ Args a, const LaunchCtl ctl) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = shared_address(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* turns = smem_raw + (base - raw) + C::kStages * C::kStageBytes;
-    Control& c = *reinterpret_cast<Control*>(turns + C::kTurnBytes);
+    Control& c = *reinterpret_cast<Control*>(turns + C::kTurns);
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
 
     if (warp == 0 && lane == 0) {
@@ -610,7 +595,7 @@ ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         }
         for (uint32_t i = 0; i < 2; ++i) {
             mbar_init(shared_address(&c.done[i]), 1);
-            mbar_init(shared_address(&c.free_[i]), 2 * kReaderWarps);
+            mbar_init(shared_address(&c.free_[i]), 2 * C::kReaders);
         }
         c.gave_up = 0;
         mbar_init_fence();
@@ -746,12 +731,12 @@ cudaError_t launch_kernel(const CUtensorMap (&maps)[4], const Args& a, uint64_t 
     const cudaError_t e = opt_in_shared_memory(reinterpret_cast<const void*>(kernel), C::kSharedBytes);
     if (e != cudaSuccess) return e;
     const uint32_t pairs = items < kPairs ? static_cast<uint32_t>(items) : kPairs;
-    return launch_chained(kernel, 2 * pairs, kThreads, C::kSharedBytes, 0, stream, maps[0], maps[1], maps[2], maps[3], a, ctl);
+    return launch_chained(kernel, 2 * pairs, C::kThreads, C::kSharedBytes, 0, stream, maps[0], maps[1], maps[2], maps[3], a, ctl);
 }
 
-template <typename T, bool BACKWARD, uint32_t COLS>
+template <typename T, bool BACKWARD, uint32_t COLS, uint32_t READERS>
 cudaError_t launch_gate_of(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
-    using C = Config<true, BACKWARD, COLS, T>;
+    using C = Config<true, BACKWARD, COLS, READERS, T>;
     a.tiles = make_tiles(a.tiles.rows, tiles_of(a.p.f, COLS / 2));
     if (!make_operand_map(&maps[2], wg, a.p.dtype, COLS / 2) || !make_operand_map(&maps[3], wu, a.p.dtype, COLS / 2)) return cudaErrorInvalidValue;
     const uint64_t items = static_cast<uint64_t>(a.tiles.rows) * a.tiles.cols;
@@ -761,12 +746,15 @@ cudaError_t launch_gate_of(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg,
 }
 template <typename T, bool BACKWARD>
 cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
-    if constexpr (sizeof(T) == 4) {
-        return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
-    } else {
-        if (gate_cols(a.tiles.rows, a.p.f) == 256) return launch_gate_of<T, BACKWARD, 256>(maps, a, wg, wu, ctl, stream);
-        return launch_gate_of<T, BACKWARD, 128>(maps, a, wg, wu, ctl, stream);
+    if (sizeof(T) == 4 || gate_cols(a.tiles.rows, a.p.f) == 128) return launch_gate_of<T, BACKWARD, 128, 8>(maps, a, wg, wu, ctl, stream);
+    if constexpr (sizeof(T) == 2) {
+        // Four reading warps for each quarter of an SM do a tile's arithmetic sooner than two, which shows where the
+        // products are short (forward 4000 x 512 x 1408: 16.3 us against 20.9); where they hide it, two do with less
+        // power, which is what bounds the clock there (8192 x 4096 x 10944: 1000 us against 1028; 2048 wide: no difference).
+        if (a.steps < 24) return launch_gate_of<T, BACKWARD, 256, 16>(maps, a, wg, wu, ctl, stream);
+        return launch_gate_of<T, BACKWARD, 256, 8>(maps, a, wg, wu, ctl, stream);
     }
+    return cudaErrorInvalidValue;
 }
 
 template <typename T>
@@ -833,7 +821,7 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
         !make_operand_map(&maps[3], wu, p.dtype, kStep))
         return cudaErrorInvalidValue;
     const uint64_t items = static_cast<uint64_t>(items_of(a.dx)) + items_of(a.dw);
-    e = launch_kernel<Config<false, false, product_cols(sizeof(T)), T>, T, 0>(maps, a, items, ctl, stream);
+    e = launch_kernel<Config<false, false, product_cols(sizeof(T)), 8, T>, T, 0>(maps, a, items, ctl, stream);
     if (e == cudaSuccess && p.dx != nullptr && a.dx.splits > 1) e = join<T>(a.dx, p.dx, nullptr, p.ld_dx, p.m, p.k, stream);
     if (e == cudaSuccess && p.dwg != nullptr && a.dw.splits > 1) e = join<T>(a.dw, p.dwg, p.dwu, p.ld_dw, p.f, p.k, stream);
     return e;
