@@ -37,11 +37,6 @@ constexpr uint32_t kTileRows = 256;
 constexpr uint32_t kBand = 16;                       // tile rows that are walked together
 constexpr uint32_t kMaxStages = 9;
 
-template <typename T> struct Planes { static constexpr uint32_t count = 1, products = 1; };
-template <> struct Planes<float> { static constexpr uint32_t count = 3, products = 6; };
-// Planes of A and of B in the parts of the reduction (4 bits each, the first part lowest).
-constexpr uint32_t kPlaneOfA = 0x010120u, kPlaneOfB = 0x001102u;
-
 // Warp-private block of shared memory through which 32 x 32 elements turn: a thread has a row of them in registers,
 // memory wants neighbouring threads on neighbouring columns.  The 16-byte pieces of a row are swapped by the row's number
 // so that neither side meets a bank conflict.
@@ -198,19 +193,6 @@ __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, in
 __device__ __forceinline__ void store32(void* to, const uint32_t (&w)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
-
-// The three bf16 planes of a float, cut off so that the two upper ones never round up to infinity.  What is not
-// finite goes into the first plane alone.
-__device__ __forceinline__ void split3(float v, uint32_t (&planes)[3]) {
-    const uint32_t bits = __float_as_uint(v);
-    const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
-    const uint32_t high = finite || (bits & 0x007fffffu) == 0 ? bits & 0xffff0000u : 0x7fc00000u;
-    const float rest = finite ? v - __uint_as_float(high) : 0.0f;
-    const uint32_t middle = __float_as_uint(rest) & 0xffff0000u;
-    planes[0] = high >> 16;
-    planes[1] = middle >> 16;
-    planes[2] = pack2<__nv_bfloat16>(rest - __uint_as_float(middle), 0.0f) & 0xffffu;
 }
 
 // Eight neighbouring elements of the thread's row of the turning block.
@@ -804,14 +786,10 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
     GateArgs g{p, make_tiles(tiles_of(p.m, kTileRows), 1), tiles_of(p.k, kStep), {reinterpret_cast<uint16_t*>(ws + l.grads), pitch}};
     if (!make_operand_map(&maps[0], x, p.dtype, 128)) return cudaErrorInvalidValue;
     maps[1] = maps[0];
-    if (sizeof(T) == 2 && p.m <= kFewRows) {
-        FfnProblem few = p;
-        few.x = x.p, few.wg = wg.p, few.wu = wu.p;
-        few.ld_x = x.ld, few.ld_wg = wg.ld, few.ld_wu = wu.ld;
-        e = launch_ffn_stream(few, backward ? ws + l.grads : nullptr, pitch, ctl, stream);
-    } else {
+    if (p.m <= kFewRows)
+        e = launch_ffn_stream(p, x, wg, wu, backward ? ws + l.grads : nullptr, pitch, ctl, stream);
+    else
         e = backward ? launch_gate<T, true>(maps, g, wg, wu, ctl, stream) : launch_gate<T, false>(maps, g, wg, wu, ctl, stream);
-    }
     if (e != cudaSuccess || !backward) return e;
 
     ProductsArgs a{p, l.dx, l.dw};

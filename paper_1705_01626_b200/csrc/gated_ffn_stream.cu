@@ -1,5 +1,4 @@
-// G and U of the gated feed-forward block for few rows of 2-byte elements (a decoding step, a short prompt), and from
-// them h or, in the backward pass, dG and dU: bound by the bytes of the weights, so the kernel is a stream of the weights through shared memory into the matrix
+// G and U of the gated feed-forward block for few rows (a decoding step, a short prompt), and from them h or, in the backward pass, dG and dU: bound by the bytes of the weights, so the kernel is a stream of the weights through shared memory into the matrix
 // units, each element read once.
 //
 // The weights are operand A: 64 rows of Wg and the same 64 of Wu are the 128 rows of a tile, the rows of x, rounded
@@ -11,6 +10,10 @@
 //
 // G of an element is in another lane of tensor memory than its U, so the accumulators pass through shared memory,
 // which also turns them: neighbouring threads then store neighbouring hidden columns of one row of h.
+//
+// 4-byte elements come as bf16 planes; a step brings all three of each operand and takes their six products.  As the
+// matrix unit cuts its sums off, the products of the high planes go round several accumulators, a few steps to each,
+// and the small ones have one of their own.
 #include "chained_launch.cuh"
 #include "gated_ffn.cuh"
 #include "gated_ffn_maps.cuh"
@@ -22,7 +25,7 @@ namespace {
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kStep = 64;
 constexpr uint32_t kTile = 64;                             // hidden columns
-constexpr uint32_t kWeightBytes = 2 * kTile * kStep * 2;   // of a step: Wg's rows, then Wu's
+constexpr uint32_t kWeightBytes = 2 * kTile * kStep * 2;   // of a step and plane: Wg's rows, then Wu's
 constexpr uint32_t kMaxStages = 12;
 constexpr uint32_t kPitch = 2 * kTile + 4;                 // floats per row of x in the turned accumulator
 
@@ -34,7 +37,8 @@ struct __align__(8) Control {
 struct StreamArgs {
     FfnProblem p;
     uint32_t steps, splits, cols, columns, stages;     // cols: rows of x, rounded up; columns: of tensor memory
-    void* grads;                                       // backward: dG, then dU, m rows of ld_grad
+    uint32_t accumulators;                             // 4-byte elements: one for the small products, then the others
+    void* grads;                                       // backward: dG, then dU, each in its planes, m rows of ld_grad
     uint64_t ld_grad;
 };
 
@@ -54,7 +58,8 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     const uint32_t warp = threadIdx.x >> 5, lane = lane_id();
     const uint32_t rank = blockIdx.x % a.splits, f0 = blockIdx.x / a.splits * kTile;
     const uint32_t first = a.steps * rank / a.splits, last = a.steps * (rank + 1) / a.splits;
-    const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
+    constexpr uint32_t kPlanes = Planes<T>::count;
+    const uint32_t x_bytes = a.cols * kStep * 2, stage_bytes = kPlanes * (kWeightBytes + x_bytes);
     const FfnProblem& p = a.p;
 
     if (threadIdx.x == 0) {
@@ -86,9 +91,12 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
             if (elect_one()) {
                 mbar_expect(bar, stage_bytes);
-                tma_load(dst, &map_wg, s * kStep, f0, 0, bar);
-                tma_load(dst + kWeightBytes / 2, &map_wu, s * kStep, f0, 0, bar);
-                tma_load(dst + kWeightBytes, &map_x, s * kStep, 0, 0, bar);
+#pragma unroll
+                for (uint32_t i = 0; i < kPlanes; ++i) {
+                    tma_load(dst + i * kWeightBytes, &map_wg, s * kStep, f0, i, bar);
+                    tma_load(dst + i * kWeightBytes + kWeightBytes / 2, &map_wu, s * kStep, f0, i, bar);
+                    tma_load(dst + kPlanes * kWeightBytes + i * x_bytes, &map_x, s * kStep, 0, i, bar);
+                }
             }
             __syncwarp();
             if (++stage == a.stages) { stage = 0; phase ^= 1u; }
@@ -102,9 +110,18 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             tcgen05_fence_after();
             const uint32_t at = base + stage * stage_bytes;
             if (elect_one()) {
+                const uint32_t n = s - first, others = a.accumulators - 1;
 #pragma unroll
-                for (uint32_t i = 0; i < kStep / 16; ++i)
-                    mma_single(tmem, operand_desc(at + 32 * i, 16, 1024), operand_desc(at + kWeightBytes + 32 * i, 16, 1024), desc, s != first || i != 0);
+                for (uint32_t q = 0; q < Planes<T>::products; ++q) {
+                    const uint32_t of_a = at + (sizeof(T) == 4 ? kPlaneOfA >> (4 * q) & 15u : 0) * kWeightBytes;
+                    const uint32_t of_b = at + kPlanes * kWeightBytes + (sizeof(T) == 4 ? kPlaneOfB >> (4 * q) & 15u : 0) * x_bytes;
+                    const bool high = sizeof(T) == 4 && q == Planes<T>::products - 1;
+                    const uint32_t to = tmem + (high ? (1 + n % others) * a.cols : 0);
+                    const bool more = high ? n >= others : n != 0 || q != 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < kStep / 16; ++i)
+                        mma_single(to, operand_desc(of_a + 32 * i, 16, 1024), operand_desc(of_b + 32 * i, 16, 1024), desc, more || i != 0);
+                }
                 mma_commit_single(shared_address(&c.empty[stage]));
             }
             __syncwarp();
@@ -123,6 +140,15 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             uint32_t v[16];
             tmem_load16(c.tmem + ((warp & 3u) * 32u << 16) + col, v);
             tmem_load_wait();
+            if constexpr (sizeof(T) == 4) {
+                for (uint32_t other = 1; other < min(a.accumulators, last - first + 1); ++other) {
+                    uint32_t w[16];
+                    tmem_load16(c.tmem + ((warp & 3u) * 32u << 16) + other * a.cols + col, w);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+                }
+            }
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) turned[(col + i) * kPitch + (warp & 3u) * 32 + lane] = __uint_as_float(v[i]);
         }
@@ -153,12 +179,24 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row, (f0 + j) >> 3) >> (j & 7u) : 1u;
         if (BACKWARD) {
             float dg, du;
-            gated_gradients<ACT, true>(g, u, to_float(static_cast<const T*>(p.dh)[row * p.ld_h + f0 + j]), keep & 1u, p.drop.scale, &dg, &du);
-            T* to = static_cast<T*>(a.grads) + row * a.ld_grad + f0 + j;
-            to[0] = from_float<T>(dg);
-            to[p.m * a.ld_grad] = from_float<T>(du);
+            gated_gradients<ACT, sizeof(T) == 2>(g, u, to_float(static_cast<const T*>(p.dh)[row * p.ld_h + f0 + j]), keep & 1u, p.drop.scale, &dg, &du);
+            const uint64_t plane = p.m * a.ld_grad;
+            uint16_t* to = static_cast<uint16_t*>(a.grads) + row * a.ld_grad + f0 + j;
+            if constexpr (sizeof(T) == 4) {
+                uint32_t of_g[3], of_u[3];
+                split3(dg, of_g);
+                split3(du, of_u);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    to[i * plane] = static_cast<uint16_t>(of_g[i]);
+                    to[(3 + i) * plane] = static_cast<uint16_t>(of_u[i]);
+                }
+            } else {
+                *reinterpret_cast<T*>(to) = from_float<T>(dg);
+                *reinterpret_cast<T*>(to + plane) = from_float<T>(du);
+            }
         } else {
-            static_cast<T*>(p.h)[row * p.ld_h + f0 + j] = from_float<T>(gated_value<ACT, true>(g, u, keep & 1u, p.drop.scale));
+            static_cast<T*>(p.h)[row * p.ld_h + f0 + j] = from_float<T>(gated_value<ACT, sizeof(T) == 2>(g, u, keep & 1u, p.drop.scale));
         }
     }
     __syncthreads();
@@ -175,33 +213,35 @@ cudaError_t launch_kernel(const CUtensorMap (&maps)[3], const StreamArgs& a, uin
 }
 
 template <typename T>
-cudaError_t launch_type(const FfnProblem& p, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream) {
+cudaError_t launch_type(const FfnProblem& p, const Matrix& x, const Matrix& wg, const Matrix& wu, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream) {
     StreamArgs a{};
     a.p = p;
     a.grads = grads;
     a.ld_grad = ld_grad;
     a.steps = tiles_of(p.k, kStep);
     a.cols = (p.m + 15) & ~15u;
+    a.accumulators = sizeof(T) == 4 ? (512 / a.cols < 8 ? 512 / a.cols : 8) : 1;
     a.columns = 32;
-    while (a.columns < a.cols) a.columns *= 2;
-    // CTAs for at most two rounds of SMs, each with steps enough to fill its ring once
+    while (a.columns < a.accumulators * a.cols) a.columns *= 2;
+    // CTAs for at most two rounds of SMs, each with four steps at least.  (So a cluster's CTAs have 72 KB of shared memory
+    // or more, at most three lie on an SM, and their tensor memory -- 128 columns at most, 512 where the ring of 4-byte
+    // elements keeps an SM to itself -- never has to wait for another cluster's.)
     const uint32_t tiles = tiles_of(p.f, kTile);
     a.splits = 1;
     while (a.splits < 8 && tiles * a.splits * 2 <= 296 && a.steps / (a.splits * 2) >= 4) a.splits *= 2;
     // One CTA to an SM may take all of its shared memory, else two share it -- not quite all of it: what waits in the
     // memory system delays the next launch's first steps (1 x 4096 x 10944: five steps of 18 KB 33.2 us, four 34.1, six
     // 36.9, twelve on an SM of its own 43.8).
-    const uint32_t stage_bytes = kWeightBytes + a.cols * kStep * 2;
-    const uint32_t room = tiles * a.splits <= 148 ? 220 * 1024 : 96 * 1024;
+    const uint32_t stage_bytes = Planes<T>::count * (kWeightBytes + a.cols * kStep * 2);
+    const uint32_t room = sizeof(T) == 4 || tiles * a.splits <= 148 ? 220 * 1024 : 96 * 1024;
     a.stages = room / stage_bytes < kMaxStages ? room / stage_bytes : kMaxStages;
     const uint32_t least = tiles_of(a.cols * kPitch * 4, stage_bytes);      // room for the turned accumulator
     const uint32_t most = tiles_of(a.steps, a.splits);
     if (a.stages > most) a.stages = most;
     const uint32_t ring = (a.stages > least ? a.stages : least) * stage_bytes;
     CUtensorMap maps[3];
-    if (!make_operand_map(&maps[0], {p.x, p.m, p.k, p.ld_x, 1}, p.dtype, a.cols) ||
-        !make_operand_map(&maps[1], {p.wg, p.f, p.k, p.ld_wg, 1}, p.dtype, kTile) ||
-        !make_operand_map(&maps[2], {p.wu, p.f, p.k, p.ld_wu, 1}, p.dtype, kTile))
+    if (!make_operand_map(&maps[0], x, p.dtype, a.cols) || !make_operand_map(&maps[1], wg, p.dtype, kTile) ||
+        !make_operand_map(&maps[2], wu, p.dtype, kTile))
         return cudaErrorInvalidValue;
     const uint32_t smem = ring + 1024;
     if (p.activation == CDMA_ACT_RELU) return launch_kernel<T, CDMA_ACT_RELU>(maps, a, tiles, smem, ctl, stream);
@@ -211,9 +251,11 @@ cudaError_t launch_type(const FfnProblem& p, void* grads, uint64_t ld_grad, cons
 
 }  // namespace
 
-cudaError_t launch_ffn_stream(const FfnProblem& p, void* grads, uint64_t ld_grad, const LaunchCtl& ctl, cudaStream_t stream) {
-    return p.dtype == CDMA_F16 ? launch_type<__half>(p, grads, ld_grad, ctl, stream)
-                               : launch_type<__nv_bfloat16>(p, grads, ld_grad, ctl, stream);
+cudaError_t launch_ffn_stream(const FfnProblem& p, const Matrix& x, const Matrix& wg, const Matrix& wu, void* grads, uint64_t ld_grad,
+                              const LaunchCtl& ctl, cudaStream_t stream) {
+    if (p.dtype == CDMA_F32) return launch_type<float>(p, x, wg, wu, grads, ld_grad, ctl, stream);
+    return p.dtype == CDMA_F16 ? launch_type<__half>(p, x, wg, wu, grads, ld_grad, ctl, stream)
+                               : launch_type<__nv_bfloat16>(p, x, wg, wu, grads, ld_grad, ctl, stream);
 }
 
 }  // namespace cdma
