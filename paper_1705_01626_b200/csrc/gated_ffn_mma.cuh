@@ -285,6 +285,31 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
             tmem_load8(g + c + 8, next_g);
             tmem_load8(u + c + 8, next_u);
         }
+        if constexpr (BACKWARD && ACT == CDMA_ACT_RELU && sizeof(T) == 2) {
+            // signs that the matrix unit may have got wrong
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(__uint_as_float(gw[j])));
+            uint32_t near = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = fabsf(__uint_as_float(gw[j]));
+                near |= (v < top * kNearZero && v != 0.0f && col + c + j < p.f ? 1u : 0u) << j;
+            }
+            if (lane_id() >= rows) near = 0;
+            uint32_t who = __ballot_sync(0xffffffffu, near != 0);
+            for (uint32_t n = 0; who != 0 && n < kRechecks; ++n) {
+                const uint32_t from = __ffs(who) - 1, j = __ffs(__shfl_sync(0xffffffffu, near, from)) - 1;
+                const float again = warp_dot(static_cast<const T*>(p.x) + static_cast<uint64_t>(row + from) * p.ld_x,
+                                             static_cast<const T*>(p.wg) + static_cast<uint64_t>(col + c + j) * p.ld_wg, p.k);
+                if (lane_id() == from) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) gw[i] = i == j ? __float_as_uint(again) : gw[i];
+                    near &= near - 1;
+                }
+                who = __ballot_sync(0xffffffffu, near != 0);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float gv = __uint_as_float(gw[j]), uv = __uint_as_float(uw[j]);

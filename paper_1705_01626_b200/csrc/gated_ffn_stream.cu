@@ -165,7 +165,6 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     const uint32_t rows = (p.m + a.splits - 1 - rank) / a.splits, at = base;
     for (uint32_t e = threadIdx.x; e < rows * kTile; e += kThreads) {
         const uint32_t row = rank + a.splits * (e / kTile), j = e % kTile;
-        if (f0 + j >= p.f) continue;
         float g = 0.0f, u = 0.0f;
         if (a.splits == 1) {
             g = turned[row * kPitch + j];
@@ -176,6 +175,20 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
                 u += load_from_cta(at + (row * kPitch + kTile + j) * 4, s);
             }
         }
+        if constexpr (BACKWARD && ACT == CDMA_ACT_RELU && sizeof(T) == 2) {
+            // signs that the matrix unit may have got wrong; a warp has 32 columns of one row
+            float top = fabsf(g);
+#pragma unroll
+            for (uint32_t d = 16; d != 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            uint32_t who = __ballot_sync(0xffffffffu, fabsf(g) < top * kNearZero && g != 0.0f && f0 + j < p.f);
+            for (uint32_t n = 0; who != 0 && n < kRechecks; ++n, who &= who - 1) {
+                const uint32_t from = __ffs(who) - 1;
+                const float again = warp_dot(static_cast<const T*>(p.x) + static_cast<uint64_t>(row) * p.ld_x,
+                                             static_cast<const T*>(p.wg) + static_cast<uint64_t>(f0 + j - lane + from) * p.ld_wg, p.k);
+                if (lane == from) g = again;
+            }
+        }
+        if (f0 + j >= p.f) continue;
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row, (f0 + j) >> 3) >> (j & 7u) : 1u;
         if (BACKWARD) {
             float dg, du;

@@ -277,3 +277,23 @@ def test_error_as_a_whole_at_ordinary_sizes(dtype):
     got, want = b.backward(), gf.backward(b.x, b.wg, b.wu, b.dh, "silu").value
     for n in got:
         assert rel(got[n], want[n]) < math.sqrt(2) * gf.UNIT[dtype] + 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("m", [128, 512])
+def test_signs_of_gates_near_zero(dtype, m):
+    # The gradient of a ReLU passes where G > 0.  x ends in the unit matrix and Wg and Wu in zeros there, so that the last
+    # columns of dWg are dG itself.  The products are of size 2^-6 and their partial sums mostly below 1: added to nearest
+    # in 32 bits, 128 to a lane and then across lanes, they are off by sqrt(133) 2^-26 = 1.7e-7 or so; a sum cut off 256
+    # times is off by more than 1e-6.  Farther from zero than 2^-21 = 4.8e-7 every sign has to be that of the sum in 64 bits.
+    k, f = 4096, 8192
+    b = Block(m, k + m, f, dtype, "relu")
+    b.x[:, k:] = torch.eye(m, device="cuda")
+    b.wg[:, k:], b.wu[:, k:] = 0, 0
+    b.dh.fill_(1.0)
+    g = b.x[:, :k].double() @ b.wg[:, :k].double().t()
+    u = b.x[:, :k].double() @ b.wu[:, :k].double().t()
+    dg = b.backward(dx=False)["dwg"][:, k:].t()
+    sure = (g.abs() > 2.0 ** -21) & (u.abs() > 2.0 ** -10)
+    assert sure.double().mean() > 0.99
+    assert torch.equal((dg != 0)[sure], (g > 0)[sure])
