@@ -115,6 +115,13 @@ def test_past_thirty_two_bits():
     assert B.cdma_dropout(x.data_ptr(), 0, 0, 0, rows, 16, B.BF16, 0.5, 11, 12, x.data_ptr(), 0, 0) == B.OK
     tail = (x[rows * 16 - 1600: rows * 16].float() / 2).cpu().numpy().reshape(100, 16)
     assert np.array_equal(tail, dn.keep_mask(100, 16, 0.5, 11, 12, first_row=rows - 100))
+    for cols in (1001, 9):                # rows that do not start on 16 bytes, long and short ones
+        x.fill_(1.0)
+        rows = n // cols
+        assert B.cdma_dropout(x.data_ptr(), 0, 0, 0, rows, cols, B.BF16, 0.5, 11, 12, x.data_ptr(), 0, 0) == B.OK
+        tail = (x[(rows - 100) * cols: rows * cols].float() / 2).cpu().numpy().reshape(100, cols)
+        assert np.array_equal(tail, dn.keep_mask(100, cols, 0.5, 11, 12, first_row=rows - 100))
+        assert (x[rows * cols:] == 1.0).all()
 
 
 def test_dropped_maps_go_through_the_codec():
