@@ -1,0 +1,129 @@
+"""Training steps of one gated feed-forward block whose hidden map is offloaded, compressed, between the two passes.
+
+    h = dropout(relu(x Wg^T) * (x Wu^T))         cdma_gated_ffn_forward: one kernel, G and U never in memory
+    offload h                                    cdma_offload_async: zero-value compression, copy to pinned memory
+    y = x + dropout(h Wd^T)                      torch product, then cdma_dropout with the residual
+    backward:
+    dz = dropout's gradient of dy                cdma_dropout_backward: the mask is computed again
+    dh = dz Wd
+    prefetch h; dWd = dz^T h                     cdma_prefetch_async
+    dx, dWg, dWu                                 cdma_gated_ffn_backward: G and U are computed again
+
+Half of h is zero behind the ReLU and the dropped elements come on top, so the map crosses the host link at less than
+half its size; nothing else of the block is kept for the backward pass.
+
+Run:  python examples/gated_ffn_training_step.py [--tokens N] [--width N] [--hidden N] [--steps N]
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_1705_01626_b200 import binding as B  # noqa: E402
+
+
+def check(r: int, where: str) -> int:
+    """Both conventions of the library: a status > 0, or a negative one in place of a byte count."""
+    if r < 0:
+        raise B.CdmaError(r, where)
+    return r
+
+
+def check_status(st: int, where: str) -> None:
+    if st != B.OK:
+        raise B.CdmaError(st, where)
+
+
+class GatedFfn:
+    """The block, its workspaces and its offload context: what a program keeps from step to step."""
+
+    def __init__(self, tokens: int, width: int, hidden: int, p: float, seed: int = 1, dtype=torch.bfloat16):
+        self.code = {torch.float32: B.F32, torch.float16: B.F16, torch.bfloat16: B.BF16}[dtype]
+        self.m, self.k, self.f, self.p, self.seed, self.dtype = tokens, width, hidden, p, seed, dtype
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        weight = lambda rows, cols: (torch.randn(rows, cols, generator=g, device="cuda") * cols ** -0.5).to(dtype)
+        self.wg, self.wu, self.wd = weight(hidden, width), weight(hidden, width), weight(width, hidden)
+        self.desc = B.cdma_gated_ffn_desc(m=tokens, k=width, f=hidden, dtype=self.code, activation=B.ACT_RELU, dropout_p=p,
+                                          dropout_seed=seed)
+        sizes = [B.cdma_gated_ffn_workspace_bytes(self.desc, backward) for backward in (0, 1)]
+        self.ws = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+        n = tokens * hidden
+        payload = B.cdma_zvc_max_compressed_bytes(n, self.code)
+        slot = payload + 8 * B.cdma_zvc_table_entries(n) + B.cdma_zvc_workspace_bytes(n, self.code) + 4096
+        self.ctx = B.cdma_ctx_create(2 * slot, 2 * slot)
+        self.h = torch.empty(tokens, hidden, dtype=dtype, device="cuda")
+
+    def close(self):
+        B.cdma_ctx_destroy(self.ctx)
+
+    def forward(self, x: torch.Tensor, step: int):
+        """Returns y and the ticket of the offloaded hidden map."""
+        stream = torch.cuda.current_stream().cuda_stream
+        self.desc.dropout_sequence = 2 * step
+        check(B.cdma_gated_ffn_forward(self.desc, x.data_ptr(), self.wg.data_ptr(), self.wu.data_ptr(), self.h.data_ptr(),
+                                       self.ws.data_ptr(), self.ws.numel(), stream), "cdma_gated_ffn_forward")
+        st, ticket = B.cdma_offload_async(self.ctx, self.h.data_ptr(), self.h.numel(), self.code, B.NCHW, stream)
+        check_status(st, "cdma_offload_async")
+        z = self.h @ self.wd.t()
+        y = torch.empty_like(x)
+        check_status(B.cdma_dropout(z.data_ptr(), self.k, x.data_ptr(), self.k, self.m, self.k, self.code, self.p, self.seed,
+                                    2 * step + 1, y.data_ptr(), self.k, stream), "cdma_dropout")
+        return y, ticket
+
+    def backward(self, x: torch.Tensor, dy: torch.Tensor, ticket, step: int):
+        """Gradients of x, Wg, Wu and Wd."""
+        stream = torch.cuda.current_stream().cuda_stream
+        self.desc.dropout_sequence = 2 * step
+        h = torch.empty_like(self.h)
+        check_status(B.cdma_prefetch_async(self.ctx, ticket, h.data_ptr(), stream), "cdma_prefetch_async")
+        dz = torch.empty_like(dy)
+        check_status(B.cdma_dropout_backward(dy.data_ptr(), self.k, self.m, self.k, self.code, self.p, self.seed, 2 * step + 1,
+                                             dz.data_ptr(), self.k, stream), "cdma_dropout_backward")
+        dh = dz @ self.wd
+        dwd = dz.t() @ h
+        dx, dwg, dwu = torch.empty_like(x), torch.empty_like(self.wg), torch.empty_like(self.wu)
+        check(B.cdma_gated_ffn_backward(self.desc, x.data_ptr(), self.wg.data_ptr(), self.wu.data_ptr(), dh.data_ptr(), dx.data_ptr(),
+                                        dwg.data_ptr(), dwu.data_ptr(), self.ws.data_ptr(), self.ws.numel(), stream),
+              "cdma_gated_ffn_backward")
+        check_status(B.cdma_ctx_synchronize(self.ctx), "cdma_ctx_synchronize")
+        return dx + dy, dwg, dwu, dwd
+
+    def update(self, grads, rate: float):
+        for w, g in zip((self.wg, self.wu, self.wd), grads):
+            w.sub_(g, alpha=rate)
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--tokens", type=int, default=4096)
+    ap.add_argument("--width", type=int, default=1024)
+    ap.add_argument("--hidden", type=int, default=2752)
+    ap.add_argument("--steps", type=int, default=5)
+    ap.add_argument("--dropout", type=float, default=0.1)
+    a = ap.parse_args(argv)
+    block = GatedFfn(a.tokens, a.width, a.hidden, a.dropout)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn(a.tokens, a.width, generator=g, device="cuda").to(block.dtype)
+    target = torch.randn(a.tokens, a.width, generator=g, device="cuda").to(block.dtype)
+    losses = []
+    for step in range(a.steps):
+        y, ticket = block.forward(x, step)
+        st, payload, _ = B.cdma_ticket_info(block.ctx, ticket)
+        check_status(st, "cdma_ticket_info")
+        off = y.float() - target.float()
+        losses.append(float(off.square().mean()))
+        _, dwg, dwu, dwd = block.backward(x, (off * (2.0 / a.width)).to(block.dtype), ticket, step)
+        block.update((dwg, dwu, dwd), rate=0.5 / a.tokens)
+        dense = block.h.numel() * block.h.element_size()
+        print("step %d  loss %.5f  hidden map %.1f MB, %.1f MB over the host link (%.2f)"
+              % (step, losses[-1], dense / 1e6, payload / 1e6, dense / payload))
+    block.close()
+    return losses
+
+
+if __name__ == "__main__":
+    main()

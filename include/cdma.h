@@ -362,7 +362,8 @@ uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int bac
 
 /*
  * Forward: h = D act(G) U with G = x Wg^T, U = x Wu^T and D the dropout factors of
- * h's elements (elementwise products).  G and U never reach memory.
+ * h's elements (elementwise products).  G and U never reach memory.  Behind a closed
+ * ReLU gate and where dropped, h is +0, which is what the codec takes for zero.
  *
  * Backward: from x, Wg, Wu and dh, with e = D dh: dU = e act(G), dG = e U act'(G),
  * dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.  G and U are computed again from the

@@ -74,14 +74,15 @@ template <int ACT, bool FAST>
 __device__ __forceinline__ float gated_value(float g, float u, bool keep, float scale) {
     float a, slope;
     activate_slope<ACT, FAST>(g, &a, &slope);
-    const float v = a * u * scale;
+    float v = a * u * scale;
+    if (ACT == CDMA_ACT_RELU) v += 0.0f;      // a closed gate times a negative U is -0, which the codec would keep: make it +0
     return keep ? v : 0.0f;
 }
 template <int ACT, bool FAST>
 __device__ __forceinline__ void gated_gradients(float g, float u, float dh, bool keep, float scale, float* dg, float* du) {
     float a, slope;
     activate_slope<ACT, FAST>(g, &a, &slope);
-    const float e = dh * scale, by_u = e * a, by_g = e * u * slope;
+    const float e = dh * scale, by_u = e * a, by_g = e * u * slope;      // (their zeros may have either sign)
     *du = keep ? by_u : 0.0f;
     *dg = keep ? by_g : 0.0f;
 }

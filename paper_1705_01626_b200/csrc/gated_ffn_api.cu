@@ -117,19 +117,29 @@ uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int bac
     return check_desc(desc, &drop) == CDMA_OK ? workspace_of(*desc, backward != 0) : 0;
 }
 
-int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
-                                 void* d_h, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream,
-                                 uint64_t* h_result) {
+// The checks and launches of both passes.
+static int gated_ffn_enqueue(const cdma_gated_ffn_desc* desc, bool backward, const void* x, const void* wg, const void* wu, void* h,
+                             const void* dh, void* dx, void* dwg, void* dwu, void* ws, uint64_t ws_bytes, void* cuda_stream,
+                             uint64_t* h_result, uint32_t stall_tile, uint64_t wait_limit_ns) {
     FfnProblem p;
-    const int st = make_problem(desc, false, d_x, d_wg, d_wu, d_h, nullptr, nullptr, nullptr, nullptr, d_workspace,
-                                workspace_bytes, h_result, &p);
+    const int st = make_problem(desc, backward, x, wg, wu, h, dh, dx, dwg, dwu, ws, ws_bytes, h_result, &p);
     if (st != CDMA_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
-    const LaunchCtl ctl = make_launch_ctl(h_result);
-    const cudaError_t e = p.dtype == CDMA_F32 && p.m <= kFewRows4 ? launch_ffn_rows(p, ctl, stream) : launch_ffn_mma(p, false, ctl, stream);
+    LaunchCtl ctl = make_launch_ctl(h_result);
+    ctl.stall_tile = stall_tile;
+    ctl.wait_limit_ns = wait_limit_ns;
+    const bool rows = !backward && p.dtype == CDMA_F32 && p.m <= kFewRows4;
+    const cudaError_t e = rows ? launch_ffn_rows(p, ctl, stream) : launch_ffn_mma(p, backward, ctl, stream);
     if (e != cudaSuccess) return CDMA_ERR_CUDA;
     return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+}
+
+int cdma_gated_ffn_forward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
+                                 void* d_h, void* d_workspace, uint64_t workspace_bytes, void* cuda_stream,
+                                 uint64_t* h_result) {
+    return gated_ffn_enqueue(desc, false, d_x, d_wg, d_wu, d_h, nullptr, nullptr, nullptr, nullptr, d_workspace, workspace_bytes,
+                             cuda_stream, h_result, kNoTile, kWaitLimitNs);
 }
 
 int64_t cdma_gated_ffn_forward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
@@ -142,15 +152,8 @@ int64_t cdma_gated_ffn_forward(const cdma_gated_ffn_desc* desc, const void* d_x,
 int cdma_gated_ffn_backward_async(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
                                   const void* d_dh, void* d_dx, void* d_dwg, void* d_dwu, void* d_workspace,
                                   uint64_t workspace_bytes, void* cuda_stream, uint64_t* h_result) {
-    FfnProblem p;
-    const int st = make_problem(desc, true, d_x, d_wg, d_wu, nullptr, d_dh, d_dx, d_dwg, d_dwu, d_workspace,
-                                workspace_bytes, h_result, &p);
-    if (st != CDMA_OK) return st;
-    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (p.m == 0 || p.f == 0 || p.k == 0) return without_kernels(p, h_result, stream);
-    const LaunchCtl ctl = make_launch_ctl(h_result);
-    if (launch_ffn_mma(p, true, ctl, stream) != cudaSuccess) return CDMA_ERR_CUDA;
-    return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
+    return gated_ffn_enqueue(desc, true, d_x, d_wg, d_wu, nullptr, d_dh, d_dx, d_dwg, d_dwu, d_workspace, workspace_bytes, cuda_stream,
+                             h_result, kNoTile, kWaitLimitNs);
 }
 
 int64_t cdma_gated_ffn_backward(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu,
@@ -159,6 +162,19 @@ int64_t cdma_gated_ffn_backward(const cdma_gated_ffn_desc* desc, const void* d_x
     uint64_t result[2] = {0, 0};
     const int st = cdma_gated_ffn_backward_async(desc, d_x, d_wg, d_wu, d_dh, d_dx, d_dwg, d_dwu, d_workspace,
                                                  workspace_bytes, cuda_stream, result);
+    return wait_for(st, cuda_stream, result);
+}
+
+// Test hook, deliberately not declared in cdma.h: the forward pass with one tile whose operands are never brought and a
+// short bound on the device-side waits.  Every wait is bounded, the kernel returns normally and the call reports
+// -CDMA_ERR_TIMEOUT.  stall_tile >= the number of CTAs stalls nothing.
+int64_t cdma_test_gated_ffn_stalled(const cdma_gated_ffn_desc* desc, const void* d_x, const void* d_wg, const void* d_wu, void* d_h,
+                                    void* d_workspace, uint64_t workspace_bytes, void* cuda_stream, uint32_t stall_tile,
+                                    uint64_t wait_limit_ns) {
+    if (wait_limit_ns == 0 || wait_limit_ns > kWaitLimitNs) return -static_cast<int64_t>(CDMA_ERR_INVALID_ARG);
+    uint64_t result[2] = {0, 0};
+    const int st = gated_ffn_enqueue(desc, false, d_x, d_wg, d_wu, d_h, nullptr, nullptr, nullptr, nullptr, d_workspace, workspace_bytes,
+                                     cuda_stream, result, stall_tile, wait_limit_ns);
     return wait_for(st, cuda_stream, result);
 }
 

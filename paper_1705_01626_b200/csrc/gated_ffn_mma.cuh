@@ -367,6 +367,7 @@ __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map
     const uint32_t full = in_cta(shared_address(&c.full[0]), 0), own_full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
     Ring<C::kStages> ring;
     bool fine = true;
+    if (ctl.stall_tile == blockIdx.x >> 1) return;      // test hook: nothing is ever brought
     for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
         const Item it = item_of<T>(a, index);
         const uint32_t row = it.row * kTileRows + rank * 128;

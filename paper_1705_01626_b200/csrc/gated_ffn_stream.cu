@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
         for (uint32_t s = first; s < last; ++s) {
+            if (ctl.stall_tile == blockIdx.x) break;      // test hook: nothing is ever brought
             if (!mbar_wait(shared_address(&c.empty[stage]), phase ^ 1u, &c.gave_up, ctl.wait_limit_ns)) break;
             const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
             if (elect_one()) {

@@ -133,6 +133,16 @@ def test_both_projections_in_one_weight_buffer(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_closed_gates_and_dropped_places_are_positive_zeros(dtype, m):
+    # the codec compresses bit patterns: -0 would be kept
+    h = Block(m, 96, 264, dtype, "relu", 0.25).forward()
+    zero = h == 0
+    assert 0.5 < zero.double().mean() < 0.8
+    assert not torch.signbit(h[zero]).any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m", [3, 90])
 def test_dropout_is_that_of_the_dropout_call(dtype, m):
     k, f, p = 96, 203, 0.4

@@ -61,3 +61,26 @@ def test_the_hook_without_a_silent_tile_is_an_ordinary_compression():
     # a silent last tile is nobody's predecessor: the call still succeeds
     last = (n + 8191) // 8192 - 1
     assert stalled(codec, x, last, 1_000_000) == len(want)
+
+
+@pytest.mark.parametrize("m", [40, 300])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_feed_forward_tile_that_never_gets_its_operands_ends_in_a_timeout(dtype, m):
+    import ctypes
+    k, f = 512, 640
+    x, wg, wu = (torch.randn(n, k, device="cuda").to(dtype) for n in (m, f, f))
+    h = torch.empty(m, f, dtype=dtype, device="cuda")
+    code = B.BF16 if dtype == torch.bfloat16 else B.F32
+    desc = B.cdma_gated_ffn_desc(m=m, k=k, f=f, dtype=code, activation=B.ACT_SILU)
+    ws = torch.empty(B.cdma_gated_ffn_workspace_bytes(desc, 0), dtype=torch.uint8, device="cuda")
+    hook = B.lib().cdma_test_gated_ffn_stalled
+    hook.restype = ctypes.c_int64
+    hook.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_uint64, ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64]
+    args = [ctypes.addressof(desc), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), h.data_ptr(), ws.data_ptr(), ws.numel(), 0]
+    assert hook(*args, 1, 20_000_000) == -B.ERR_TIMEOUT
+    # the context is as good as before, with the same workspace
+    want = torch.nn.functional.silu(x.double() @ wg.double().t()) * (x.double() @ wu.double().t())
+    assert hook(*args, 1 << 20, 2_000_000_000) == h.numel() * h.element_size()
+    assert ((h.double() - want).norm() / want.norm()) < 2.0 ** -8
+    assert B.cdma_gated_ffn_forward(desc, *args[1:]) == h.numel() * h.element_size()
+    assert ((h.double() - want).norm() / want.norm()) < 2.0 ** -8
