@@ -124,8 +124,13 @@ __device__ __noinline__ float warp_dot(const T* a, const T* b, uint32_t k) {
 // measured, microseconds forward, bf16: 128 rows of 4096 x 10944 43 against 65, 192 rows 108 against 65, 128 rows of
 // 1024 x 2752 14.4 either way.
 constexpr uint64_t kFewRows = 128;
-// Forward pass of few rows of 4-byte elements (gated_ffn_rows.cu).
-constexpr uint64_t kFewRows4 = 16;
+// Whether the forward pass goes through registers (gated_ffn_rows.cu).  2-byte elements, 4096 x 10944: one row 28.6 us
+// against 33.3 as a weight stream, two 31.1 against 34.4, four 48.3 against 34.1; 2049 x 5505, whose operands would have to
+// be copied for the stream, four rows: 23.3 against 29.1.  4-byte elements, 2048 x 5504, 16 rows: 60.7 against 73.
+inline bool in_registers(uint64_t m, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype) {
+    if (dtype == CDMA_F32) return m <= 16;
+    return m <= ((m == 1 || ld_x % 8 == 0) && ld_wg % 8 == 0 && ld_wu % 8 == 0 ? 2 : 4);
+}
 cudaError_t launch_ffn_rows(const FfnProblem& p, const LaunchCtl& ctl, cudaStream_t stream);
 // Any number of rows (gated_ffn_mma.cu).
 uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward);

@@ -25,9 +25,9 @@ int check_desc(const cdma_gated_ffn_desc* d, DropoutSpec* drop) {
 uint64_t or_dense(uint64_t ld, uint64_t cols) { return ld != 0 ? ld : cols; }
 
 uint64_t workspace_of(const cdma_gated_ffn_desc& d, bool backward) {
-    if (!backward && d.dtype == CDMA_F32 && d.m <= kFewRows4) return kFfnWsHeader;
-    const uint64_t bytes = ffn_mma_workspace(d.m, d.k, d.f, or_dense(d.ld_x, d.k), or_dense(d.ld_wg, d.k), or_dense(d.ld_wu, d.k),
-                                             d.dtype, backward);
+    const uint64_t ld_x = or_dense(d.ld_x, d.k), ld_wg = or_dense(d.ld_wg, d.k), ld_wu = or_dense(d.ld_wu, d.k);
+    if (!backward && in_registers(d.m, ld_x, ld_wg, ld_wu, d.dtype)) return kFfnWsHeader;
+    const uint64_t bytes = ffn_mma_workspace(d.m, d.k, d.f, ld_x, ld_wg, ld_wu, d.dtype, backward);
     return (bytes + 255) & ~255ull;
 }
 
@@ -129,7 +129,7 @@ static int gated_ffn_enqueue(const cdma_gated_ffn_desc* desc, bool backward, con
     LaunchCtl ctl = make_launch_ctl(h_result);
     ctl.stall_tile = stall_tile;
     ctl.wait_limit_ns = wait_limit_ns;
-    const bool rows = !backward && p.dtype == CDMA_F32 && p.m <= kFewRows4;
+    const bool rows = !backward && in_registers(p.m, p.ld_x, p.ld_wg, p.ld_wu, p.dtype);
     const cudaError_t e = rows ? launch_ffn_rows(p, ctl, stream) : launch_ffn_mma(p, backward, ctl, stream);
     if (e != cudaSuccess) return CDMA_ERR_CUDA;
     return finish_result(p.ws, ctl, h_result, stream) == cudaSuccess ? CDMA_OK : CDMA_ERR_CUDA;
