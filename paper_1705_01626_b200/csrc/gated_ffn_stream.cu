@@ -14,6 +14,9 @@
 // 4-byte elements come as bf16 planes; a step brings all three of each operand and takes their six products.  As the
 // matrix unit cuts its sums off, the products of the high planes go round several accumulators, a few steps to each,
 // and the small ones have one of their own.
+//
+// Bound by memory between about 5 us of start and end: 64 rows of 4096 x 10944 bf16 in 37 us, 4.9 TB/s of 6.5; 24 rows of
+// 2048 x 5504 in 14.3 us, of which the stream is 7.
 #include "chained_launch.cuh"
 #include "gated_ffn.cuh"
 #include "gated_ffn_maps.cuh"
