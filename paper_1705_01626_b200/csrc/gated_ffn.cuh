@@ -33,9 +33,20 @@ constexpr uint64_t kFfnWsHeader = 256;   // bytes in front of the rest of the wo
 // the codec does.  FAST, for results of 2-byte types: the exponential and the quotient by the hardware's
 // approximations, a few units of 2^-22 off, where the result is rounded at 2^-9 or 2^-12.
 template <bool FAST>
-__device__ __forceinline__ float exponential(float v) { return FAST ? __expf(v) : expf(v); }
+__device__ __forceinline__ float exponential(float v) {
+    if (!FAST) return expf(v);
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v * 1.4426950408889634f));
+    return e;
+}
+// 1 / d for d of 1 or more
+__device__ __forceinline__ float reciprocal(float d) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return r;
+}
 template <bool FAST>
-__device__ __forceinline__ float logistic(float g) { return __fdividef(1.0f, 1.0f + exponential<FAST>(-g)); }
+__device__ __forceinline__ float logistic(float g) { return reciprocal(1.0f + exponential<FAST>(-g)); }
 
 // The normal distribution function at g and its density, by formula 7.1.26 of Abramowitz and Stegun, "Handbook of
 // Mathematical Functions" (a polynomial of 1 / (1 + 0.3275911 z) times e^-z^2, at most 1.5e-7 off for erf): without
@@ -43,7 +54,7 @@ __device__ __forceinline__ float logistic(float g) { return __fdividef(1.0f, 1.0
 template <bool FAST>
 __device__ __forceinline__ void normal(float g, float* cdf, float* density) {
     const float e = exponential<FAST>(-0.5f * g * g);
-    const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.0f));
+    const float t = reciprocal(fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.0f));
     const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
     const float tail = 0.5f * poly * e;
     *cdf = g > 0.0f ? 1.0f - tail : tail;

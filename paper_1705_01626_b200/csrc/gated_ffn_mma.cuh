@@ -251,7 +251,7 @@ __device__ __forceinline__ void fetch_dh(uint8_t* turn, uint32_t (&words)[16], c
 
 // 32 hidden columns of the warp's 32 rows: h, or dG and dU; G at tensor-memory place `g`, U at `u`.  dh: in `words`, or
 // in the turning block for 4-byte elements.  Eight columns at
-// a time in a rolled loop: unrolled over all columns the code does not fit the instruction cache, and the first tile
+// a time, two turns unrolled: over all columns the code does not fit the instruction cache, and the first tile
 // of a launch, often its only one, waited for instructions most of the time (GELU: 37,000 cycles for 32 columns).
 template <typename T, int ACT, bool BACKWARD>
 __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, uint32_t row, uint32_t col, uint32_t g, uint32_t u,
@@ -265,7 +265,7 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
     uint32_t next_g[8], next_u[8];
     tmem_load8(g, next_g);
     tmem_load8(u, next_u);
-#pragma unroll 1
+#pragma unroll 2
     for (uint32_t c = 0; c < 32; c += 8) {
         const uint32_t keep = p.drop.threshold ? dropout_keep8(p.drop, row + lane_id(), (col + c) >> 3) : 0xffu;
         float dh[8], first[8], other[8];
@@ -291,14 +291,19 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
         }
         if constexpr (BACKWARD && ACT == CDMA_ACT_RELU && sizeof(T) == 2) {
             // signs that the matrix unit may have got wrong
-            float top = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(__uint_as_float(gw[j])));
-            uint32_t near = 0;
+            float top = 0.0f, low = INFINITY;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float v = fabsf(__uint_as_float(gw[j]));
-                near |= (v < top * kNearZero && v != 0.0f && col + c + j < p.f ? 1u : 0u) << j;
+                top = fmaxf(top, fabsf(__uint_as_float(gw[j])));
+                low = fminf(low, fabsf(__uint_as_float(gw[j])));
+            }
+            uint32_t near = 0;
+            if (low < top * kNearZero) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float v = fabsf(__uint_as_float(gw[j]));
+                    near |= (v < top * kNearZero && v != 0.0f && col + c + j < p.f ? 1u : 0u) << j;
+                }
             }
             if (lane_id() >= rows) near = 0;
             uint32_t who = __ballot_sync(0xffffffffu, near != 0);
