@@ -1,7 +1,8 @@
 // Launches that may begin before the kernel in front of them on the stream has ended (programmatic dependent launch).
 // Such a kernel sets itself up, then waits for all work in front of it -- let_next_start() and wait_for_previous()
 // are the two ends -- before it touches any memory of the caller.  A kernel that cannot begin early simply finds
-// nothing to wait for.  It hides the start of a kernel of a few microseconds behind the end of the one before.
+// nothing to wait for.  As it may have begun before its inputs were written, it must not read them through the
+// read-only path (ld.global.nc, __ldg).  It hides the start of a kernel of a few microseconds behind the end of the one before.
 #pragma once
 
 #include <cuda_runtime.h>

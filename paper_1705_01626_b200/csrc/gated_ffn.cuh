@@ -113,7 +113,7 @@ __device__ __noinline__ float warp_dot(const T* a, const T* b, uint32_t k) {
     uint32_t i = 0;
     if (((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15u) == 0) {
         for (i = 8 * lane_id(); i + 8 <= k; i += 256) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(a + i)), w = __ldg(reinterpret_cast<const uint4*>(b + i));
+            const uint4 v = *reinterpret_cast<const uint4*>(a + i), w = *reinterpret_cast<const uint4*>(b + i);
             const uint32_t vw[4] = {v.x, v.y, v.z, v.w}, ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -14,7 +14,7 @@ constexpr uint32_t kLeastSteps = 8;      // of an item: fewer would be lost in f
 Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward, bool dx, bool dw) {
     Plan l{};
     const uint64_t copy = 2 * planes_of(dtype), products = dtype == CDMA_F32 ? 6 : 1;
-    l.grads = kFfnWsHeader;
+    l.grads = 0;
     l.x = l.grads + (backward ? round256(2 * m * pitch_of(f) * copy) : 0);
     l.wg = l.x + (needs_copy(ld_x, m, dtype) ? round256(m * pitch_of(k) * copy) : 0);
     l.wu = l.wg + (needs_copy(ld_wg, f, dtype) ? round256(f * pitch_of(k) * copy) : 0);
@@ -68,7 +68,7 @@ uint64_t ffn_mma_workspace(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, ui
     const uint64_t one = plan_of(m, k, f, ld_x, ld_wg, ld_wu, dtype, backward, true, false).end;
     const uint64_t other = plan_of(m, k, f, ld_x, ld_wg, ld_wu, dtype, backward, false, true).end;
     const uint64_t most = one > other ? one : other;
-    return both > most ? both : most;
+    return kFfnWsHeader + 256 + (both > most ? both : most);      // the regions begin on 256 bytes
 }
 
 cudaError_t launch_ffn_mma(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {

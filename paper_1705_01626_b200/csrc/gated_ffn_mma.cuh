@@ -179,7 +179,7 @@ __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, in
             uint4* there = reinterpret_cast<uint4*>(at + r * ld + vector * kPer);
             uint4* here = reinterpret_cast<uint4*>(turn_at<T>(turn, r, vector));
             if (STORE) { if (r < rows) *there = *here; }
-            else *here = r < rows ? __ldg(there) : make_uint4(0, 0, 0, 0);
+            else *here = r < rows ? *there : make_uint4(0, 0, 0, 0);
         }
     } else {
 #pragma unroll 8
@@ -243,7 +243,7 @@ __device__ __forceinline__ void fetch_dh(uint8_t* turn, uint32_t (&words)[16], c
     for (int i = 0; i < 4; ++i) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (!vectors) v = *reinterpret_cast<const uint4*>(turn_at<T>(turn, lane_id(), i));
-        else if (lane_id() < rows) v = __ldg(reinterpret_cast<const uint4*>(at + lane_id() * ld) + i);
+        else if (lane_id() < rows) v = reinterpret_cast<const uint4*>(at + lane_id() * ld)[i];
         words[4 * i] = v.x; words[4 * i + 1] = v.y; words[4 * i + 2] = v.z; words[4 * i + 3] = v.w;
     }
     __syncwarp();
@@ -737,6 +737,11 @@ struct Plan {
 };
 Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, uint64_t ld_wu, int dtype, bool backward, bool dx, bool dw);
 
+// Where the plan's offsets count from: behind the result words, on 256 bytes (32-byte stores go there).
+inline uint8_t* regions_of(const FfnProblem& p) {
+    return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p.ws) + kFfnWsHeader + 255) & ~static_cast<uintptr_t>(255));
+}
+
 // Columns of a products tile: the running sums of 4-byte elements take the other half of tensor memory.
 constexpr uint32_t product_cols(uint64_t size) { return size == 4 ? 128 : 256; }
 // Hidden columns of a gate tile of 2-byte elements, times two.
@@ -784,7 +789,7 @@ cudaError_t join(const Product& q, void* out, void* out2, uint64_t ld, uint32_t 
 // Copies the operands that need it; x, wg and wu then name what the kernels read.
 template <typename T>
 cudaError_t prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matrix (&m)[3], cudaStream_t stream) {
-    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    uint8_t* ws = regions_of(p);
     m[0] = {p.x, p.m, p.k, p.ld_x, 1};
     m[1] = {p.wg, p.f, p.k, p.ld_wg, 1};
     m[2] = {p.wu, p.f, p.k, p.ld_wu, 1};
@@ -810,7 +815,7 @@ cudaError_t prepare_operands(const FfnProblem& p, const uint64_t (&at)[3], Matri
 template <typename T>
 cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl, cudaStream_t stream) {
     Plan l = plan_of(p.m, p.k, p.f, p.ld_x, p.ld_wg, p.ld_wu, p.dtype, backward, p.dx != nullptr, p.dwg != nullptr);
-    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    uint8_t* ws = regions_of(p);
     Matrix operands[3];
     cudaError_t e = prepare_operands<T>(p, {l.x, l.wg, l.wu}, operands, stream);
     if (e != cudaSuccess) return e;

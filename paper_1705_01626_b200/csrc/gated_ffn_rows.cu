@@ -33,9 +33,9 @@ __device__ __forceinline__ Raw<T> take16(const T* row, uint32_t left) {
     if constexpr (VECTORS && WHOLE) {
         const T* at = row + kCount * lane_id();
         if (STREAM) {
-            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3]) : "l"(at));
+            asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.w[0]), "=r"(q.w[1]), "=r"(q.w[2]), "=r"(q.w[3]) : "l"(at));
         } else {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(at));
+            const uint4 v = *reinterpret_cast<const uint4*>(at);
             q.w[0] = v.x; q.w[1] = v.y; q.w[2] = v.z; q.w[3] = v.w;
         }
     } else {
@@ -45,7 +45,7 @@ __device__ __forceinline__ Raw<T> take16(const T* row, uint32_t left) {
 #pragma unroll
         for (uint32_t i = 0; i < kCount; ++i) {
             const uint32_t c = VECTORS ? kCount * lane_id() + i : 32 * i + lane_id();
-            e[i] = WHOLE || c < left ? __ldg(bits + c) : 0u;
+            e[i] = WHOLE || c < left ? bits[c] : 0u;
         }
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) q.w[i] = sizeof(T) == 4 ? e[i] : e[2 * i % kCount] | e[(2 * i + 1) % kCount] << 16;

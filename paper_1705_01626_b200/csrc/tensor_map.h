@@ -31,7 +31,7 @@ inline bool encode_matrix_map(CUtensorMap* map, CUtensorMapDataType type, uint32
                               CUtensorMapSwizzle swizzle) {
     const auto encode = tensor_map_encoder();
     if (encode == nullptr) return false;
-    const cuuint64_t dims[3] = {cols, rows, planes}, strides[2] = {ld * size, plane * size};
+    const cuuint64_t dims[3] = {cols, rows, planes}, strides[2] = {ld * size, (planes > 1 ? plane : ld) * size};
     const cuuint32_t box[3] = {box_cols, box_rows, 1}, steps[3] = {1, 1, 1};
     return encode(map, type, 3, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -37,9 +37,11 @@ class Block:
             m=m, k=k, f=f, ld_x=k + pads[0], ld_wg=k + pads[1], ld_wu=k + pads[2], ld_h=f + pads[3], ld_dx=k + pads[4],
             ld_dw=k + pads[5], dtype=DT[dtype], activation=ACTS[act], dropout_p=p, dropout_seed=seed, dropout_sequence=sequence)
 
+    ws_shift = 0        # bytes of the workspace's start past 512
+
     def workspace(self, backward):
         self.ws_bytes = B.cdma_gated_ffn_workspace_bytes(self.desc, backward)
-        self.ws = torch.full((self.ws_bytes + 256,), CANARY, dtype=torch.uint8, device="cuda")
+        self.ws = torch.full((self.ws_shift + self.ws_bytes + 256,), CANARY, dtype=torch.uint8, device="cuda")[self.ws_shift:]
 
     def forward(self, stream=0):
         self.workspace(0)
@@ -168,6 +170,65 @@ def test_parts_of_the_gradient(dtype, m):
     b.dxw.fill_(7.0)
     got = b.backward(dx=False)
     assert torch.equal(got["dwg"], both["dwg"]) and torch.equal(got["dwu"], both["dwu"]) and (b.dxw == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shift", [16, 240])
+def test_workspaces_anywhere_on_sixteen_bytes(dtype, shift):
+    for m in (20, 150, 300):            # split products with sums in the workspace among them
+        b = Block(m, 1001, 520, dtype, "silu")
+        b.ws_shift = shift
+        b.check_forward()
+        b.check_backward()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 20, 300])
+def test_calls_in_a_graph(dtype, m):
+    b = Block(m, 264, 520, dtype, "relu", 0.25)
+    want, grads = b.forward().clone(), {n: t.clone() for n, t in b.backward().items()}
+    words = torch.zeros(2, dtype=torch.int64).pin_memory()
+    y = torch.empty(m, 520, dtype=dtype, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s = torch.cuda.current_stream().cuda_stream
+        assert B.cdma_gated_ffn_forward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.hw.data_ptr(),
+                                              b.ws.data_ptr(), b.ws_bytes, s, words.data_ptr()) == B.OK
+        assert B.cdma_dropout(b.hw.data_ptr(), 520, 0, 0, m, 520, DT[dtype], 0.0, 1, 2, y.data_ptr(), 520, s) == B.OK
+        assert B.cdma_gated_ffn_backward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.dh.data_ptr(),
+                                               b.dxw.data_ptr(), b.dwgw.data_ptr(), b.dwuw.data_ptr(), b.ws.data_ptr(),
+                                               b.ws_bytes, s, words.data_ptr()) == B.OK
+    for _ in range(3):
+        for t in (b.hw, y, b.dxw, b.dwgw, b.dwuw):
+            t.fill_(7.0)
+        words.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(b.hw, want) and torch.equal(y, want)
+        assert torch.equal(b.dxw, grads["dx"]) and torch.equal(b.dwgw, grads["dwg"]) and torch.equal(b.dwuw, grads["dwu"])
+        assert int(words[1]) == 0 and int(words[0]) > 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_inputs_written_right_before_the_call(dtype):
+    # launches begin before the kernel in front has ended: what that kernel writes has to be what is read
+    for m in (1, 2, 20, 300):
+        b = Block(m, 512, 1024, dtype, "silu")
+        b.workspace(0)
+        stream = torch.cuda.current_stream().cuda_stream
+        words = torch.zeros(2, dtype=torch.int64).pin_memory()
+        x, outs = b.x.clone(), []
+        for i in range(20):
+            b.x.copy_(x)
+            b.x.mul_(1.0 + i)
+            assert B.cdma_gated_ffn_forward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.hw.data_ptr(),
+                                                  b.ws.data_ptr(), b.ws_bytes, stream, words.data_ptr()) == B.OK
+            outs.append(b.hw.clone())
+        for i in (0, 7, 19):
+            b.x.copy_(x)
+            b.x.mul_(1.0 + i)
+            torch.cuda.synchronize()
+            assert torch.equal(b.forward(), outs[i])
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
