@@ -79,7 +79,8 @@ struct Gradients {      // dG then dU, each in its planes: `m` rows of `ld` 2-by
     uint64_t ld;
 };
 // Output tiles of a product, in bands of kBand tile rows, down a band's column first: the tiles that run at one time
-// then share few rows of either operand, which stay in L2.  (Divisions by numbers that the host knows: each role of a
+// then share few rows of either operand, which stay in L2 (8192 x 4096 x 10944: bands of 16 forward 978 us and backward
+// 3.26 ms, of 8 996 us and 3.23 ms, of 32 1050 us and 3.47 ms).  (Divisions by numbers that the host knows: each role of a
 // CTA goes through them for each tile, and tiles of a few steps waited for them.)
 struct Tiles {
     uint32_t rows, cols;
