@@ -48,11 +48,16 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
 }
 
 uint32_t gate_cols(uint32_t tile_rows, uint32_t f) {
-    // The choice whose rounds over the pairs cost less.  A step of 128 columns takes 350 cycles, one of 256 takes 515: the
-    // matrix unit is as long at fetching A for either (and for 64 columns).  Narrow tiles pay where wide ones leave pairs
-    // idle.
-    const auto rounds = [&](uint32_t cols) { return (static_cast<uint64_t>(tile_rows) * tiles_of(f, cols / 2) + kPairs - 1) / kPairs; };
-    return rounds(128) * 350 < rounds(256) * 515 ? 128 : 256;
+    // The choice whose rounds over the pairs cost least.  A step of 128 columns takes 350 cycles (one of 64 as well: the matrix
+    // unit is as long at fetching A for any), of 192 columns 370, of 256 490.  Narrow tiles pay where wide ones leave pairs idle.
+    uint32_t best = 256;
+    uint64_t least = ~0ull;
+    for (const uint32_t cols : {256u, 192u, 128u}) {
+        const uint64_t items = static_cast<uint64_t>(tile_rows) * tiles_of(f, cols / 2);
+        const uint64_t cycles = (items + kPairs - 1) / kPairs * (cols == 256 ? 490 : cols == 192 ? 370 : 350);
+        if (cycles < least) { least = cycles; best = cols; }
+    }
+    return best;
 }
 extern template cudaError_t launch_all<float>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);
 extern template cudaError_t launch_all<__half>(const FfnProblem&, bool, const LaunchCtl&, cudaStream_t);

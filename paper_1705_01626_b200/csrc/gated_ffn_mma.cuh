@@ -69,9 +69,10 @@ struct Config {
     static constexpr uint32_t kFit = (232448 - 1024 - sizeof(Control) - kTurns) / kStageBytes;
     static constexpr uint32_t kStages = kFit < kMaxStages ? kFit : kMaxStages;
     static constexpr uint32_t kSharedBytes = 1024 + kStages * kStageBytes + kTurns + sizeof(Control);
-    // two accumulators; 4-byte elements have their running sums beside them
-    static constexpr uint32_t kTmemCols = sizeof(T) == 4 ? 4 * COLS : 2 * COLS;
-    static_assert(kTmemCols <= 512, "tensor memory has 512 columns");
+    // two accumulators; 4-byte elements have their running sums beside them (the gate kernel's are in registers)
+    static constexpr uint32_t kTmemUsed = sizeof(T) == 4 && !GATE ? 3 * COLS : 2 * COLS;
+    static constexpr uint32_t kTmemCols = kTmemUsed <= 256 ? 256 : 512;      // allocations are powers of two
+    static_assert(kTmemUsed <= 512, "tensor memory has 512 columns");
 };
 
 struct Gradients {      // dG then dU, each in its planes: `m` rows of `ld` 2-byte elements per plane
@@ -503,16 +504,40 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             }
         }
         uint32_t from = tmem;
+        [[maybe_unused]] float sum[2][sizeof(T) == 4 && C::kGate ? 32 : 1];
         for (uint32_t s = it.first; s < it.last; ++n) {
             const uint32_t end = end_of_stretch<T>(it, s), acc = n & 1u;
             if (!(fine = mbar_wait(shared_address(&c.done[acc]), (n >> 1) & 1u, &c.gave_up, ctl.wait_limit_ns))) break;
             tcgen05_fence_after();
             __syncwarp();
             from = tmem + acc * C::kCols;
-            if constexpr (sizeof(T) == 4) {
+            if constexpr (sizeof(T) == 4 && C::kGate) {
+                // the sums of the warp's block; after the last stretch they go back for finish_gate to take piece by piece
+                constexpr uint32_t kUp = C::kCols / 2;
+                const uint32_t at = from + group * 32;
+                uint32_t v[32];
+#pragma unroll
+                for (uint32_t side = 0; side < 2; ++side) {
+                    tmem_load32(at + side * kUp, v);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[side][j] = s != it.first ? sum[side][j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
+                }
+                if (end < it.last) {
+                    tcgen05_fence_before();
+                    if (lane == 0) mbar_arrive_cluster(free0 + 8 * acc);
+                } else {
+#pragma unroll
+                    for (uint32_t side = 0; side < 2; ++side) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[side][j]);
+                        tmem_store32(at + side * kUp, v);
+                    }
+                    tmem_store_wait();
+                }
+            } else if constexpr (sizeof(T) == 4) {
 #pragma unroll 1
                 for (uint32_t i = group; i < C::kCols / 32; i += C::kGroups) {
-                    // blocks of G and of U alternate between the warps as the gate's reader takes them
                     const uint32_t at = i * 32;
                     uint32_t v[32], w[32];
                     tmem_load32(from + at, v);
@@ -529,7 +554,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             s = end;
         }
         if (!fine) break;
-        if constexpr (sizeof(T) == 4) from = sums;
+        if constexpr (sizeof(T) == 4 && !C::kGate) from = sums;
         if constexpr (C::kGate) {
 #pragma unroll
             for (uint32_t i = 0; i < kOwn; ++i) {
@@ -588,7 +613,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             }
         }
         __syncwarp();
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2 || C::kGate) {
             tcgen05_fence_before();
             if (lane == 0) mbar_arrive_cluster(free0 + 8 * ((n - 1) & 1u));
         }
@@ -769,11 +794,18 @@ cudaError_t launch_gate_of(CUtensorMap (&maps)[4], GateArgs a, const Matrix& wg,
 }
 template <typename T, bool BACKWARD>
 cudaError_t launch_gate(CUtensorMap (&maps)[4], const GateArgs& a, const Matrix& wg, const Matrix& wu, const LaunchCtl& ctl, cudaStream_t stream) {
-    if (sizeof(T) == 4 || gate_cols(a.tiles.rows, a.p.f) == 128) return launch_gate_of<T, BACKWARD, 128, 8>(maps, a, wg, wu, ctl, stream);
+    if constexpr (sizeof(T) == 4) {
+        // the sums of a 192-column tile leave its readers too few registers for the planes of dG and dU (backward 200 x 1024 x
+        // 2752: 115 us against 101; forward 1000 x 1024 x 2752: 67 against 78)
+        return launch_gate_of<T, BACKWARD, BACKWARD ? 128 : 192, BACKWARD ? 8 : 12>(maps, a, wg, wu, ctl, stream);
+    }
+    const uint32_t cols = gate_cols(a.tiles.rows, a.p.f);
     if constexpr (sizeof(T) == 2) {
         // Four reading warps for each quarter of an SM do a tile's arithmetic sooner than two, which shows where the
         // products are short (forward 4000 x 512 x 1408: 16.3 us against 20.9); where they hide it, two do with less
         // power, which is what bounds the clock there (8192 x 4096 x 10944: 1000 us against 1028; 2048 wide: no difference).
+        if (cols == 128) return launch_gate_of<T, BACKWARD, 128, 8>(maps, a, wg, wu, ctl, stream);
+        if (cols == 192) return launch_gate_of<T, BACKWARD, 192, 12>(maps, a, wg, wu, ctl, stream);
         if (a.steps < 24) return launch_gate_of<T, BACKWARD, 256, 16>(maps, a, wg, wu, ctl, stream);
         return launch_gate_of<T, BACKWARD, 256, 8>(maps, a, wg, wu, ctl, stream);
     }
