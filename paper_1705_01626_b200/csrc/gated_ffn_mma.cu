@@ -47,6 +47,26 @@ Plan plan_of(uint64_t m, uint64_t k, uint64_t f, uint64_t ld_x, uint64_t ld_wg, 
     return l;
 }
 
+// An item of dx can be many times as long as one of dW.  Handed out in turn, the pairs that begin with dx would get as many
+// of dW as the others; instead they get `own` each, the number that ends soonest.  In steps; a tile takes eight at least,
+// the time to read its accumulator.  (More items of dx than pairs: in turn, many of both to each.)
+void balance(ProductsArgs* a, uint32_t pairs) {
+    a->heavy = a->rest = 0;
+    const uint64_t of_dx = items_of(a->dx), of_dw = items_of(a->dw);
+    if (of_dx == 0 || of_dw == 0 || of_dx >= pairs) return;
+    const uint64_t light = pairs - of_dx, long_one = a->dx.share > 8 ? a->dx.share : 8, short_one = a->dw.share > 8 ? a->dw.share : 8;
+    const uint64_t more = long_one / short_one;      // items of dW that one of dx is worth
+    const uint64_t even = of_dw > light * more ? (of_dw - light * more) / pairs : 0;
+    uint64_t soonest = ~0ull, own = 0;
+    for (uint64_t n = even > 0 ? even - 1 : 0; n <= even + 1 && n * of_dx <= of_dw; ++n) {
+        const uint64_t of_heavy = long_one + n * short_one, of_light = (of_dw - n * of_dx + light - 1) / light * short_one;
+        const uint64_t end = of_heavy > of_light ? of_heavy : of_light;
+        if (end < soonest) { soonest = end; own = n; }
+    }
+    a->heavy = static_cast<uint32_t>(of_dx);
+    a->rest = static_cast<uint32_t>(of_dw - own * of_dx);
+}
+
 uint32_t gate_cols(uint32_t tile_rows, uint32_t f) {
     // The choice whose rounds over the pairs cost least.  A step of 128 columns takes 350 cycles (one of 64 as well: the matrix
     // unit is as long at fetching A for any), of 192 columns 370, of 256 490.  Narrow tiles pay where wide ones leave pairs idle.

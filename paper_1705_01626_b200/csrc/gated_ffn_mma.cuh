@@ -118,6 +118,9 @@ struct Product {
 struct ProductsArgs {
     FfnProblem p;
     Product dx, dw;
+    // With `heavy` pairs of CTAs on one item of dx each, the others share the first `rest` items of dW, the heavy ones the
+    // remaining ones (balance()).  heavy = 0: all items in turn.
+    uint32_t heavy, rest;
 };
 
 // What a pair of CTAs does at one time: an output tile and a range of its reduction.
@@ -130,8 +133,21 @@ struct Item {
     uint32_t small;           // steps of the small products of planes, which come first
 };
 
+// The items of a pair of CTAs: `first`, then every stride-th from `start` to below `end`.
+struct Walk {
+    uint32_t index, start, stride, end;
+    bool begun = false;
+    __device__ __forceinline__ bool more() const { return index < end; }
+    __device__ __forceinline__ void next() {
+        index = begun ? index + stride : start;
+        begun = true;
+    }
+};
 template <typename T>
-__device__ __forceinline__ uint32_t items_of(const GateArgs& a) { return a.tiles.rows * a.tiles.cols; }
+__device__ __forceinline__ Walk walk_of(const GateArgs& a) {
+    const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    return Walk{pair, pair + pairs, pairs, a.tiles.rows * a.tiles.cols};
+}
 template <typename T>
 __device__ __forceinline__ Item item_of(const GateArgs& a, uint32_t index) {
     Item it{};
@@ -143,7 +159,13 @@ __device__ __forceinline__ Item item_of(const GateArgs& a, uint32_t index) {
 }
 __host__ __device__ __forceinline__ uint32_t items_of(const Product& q) { return q.tiles.rows * q.tiles.cols * q.splits; }
 template <typename T>
-__device__ __forceinline__ uint32_t items_of(const ProductsArgs& a) { return items_of(a.dx) + items_of(a.dw); }
+__device__ __forceinline__ Walk walk_of(const ProductsArgs& a) {
+    const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, items = items_of(a.dx) + items_of(a.dw);
+    if (a.heavy == 0) return Walk{pair, pair + pairs, pairs, items};
+    if (pair < a.heavy) return Walk{pair, a.heavy + a.rest + pair, a.heavy, items};
+    const uint32_t light = pairs - a.heavy;
+    return Walk{pair, pair + light, light, a.heavy + a.rest};
+}
 template <typename T>
 __device__ __forceinline__ Item item_of(const ProductsArgs& a, uint32_t index) {
     Item it{};
@@ -374,13 +396,13 @@ __device__ __forceinline__ uint32_t end_of_stretch(const Item& it, uint32_t s) {
 template <typename C, typename T, typename Args>
 __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map_x, const CUtensorMap* map_g, const CUtensorMap* map_wg,
                                            const CUtensorMap* map_wu, uint32_t base, Control& c, const LaunchCtl& ctl) {
-    const uint32_t rank = cluster_rank(), items = items_of<T>(a);
+    const uint32_t rank = cluster_rank();
     const uint32_t full = in_cta(shared_address(&c.full[0]), 0), own_full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
     Ring<C::kStages> ring;
     bool fine = true;
     if (ctl.stall_tile == blockIdx.x >> 1) return;      // test hook: nothing is ever brought
-    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
-        const Item it = item_of<T>(a, index);
+    for (Walk walk = walk_of<T>(a); fine && walk.more(); walk.next()) {
+        const Item it = item_of<T>(a, walk.index);
         const uint32_t row = it.row * kTileRows + rank * 128;
         const uint32_t col = C::kGate ? it.col * (C::kCols / 2) : it.col * C::kCols + rank * (C::kCols / 2);
         uint32_t part = it.part, r = (it.first - it.part * it.steps) * kStep;
@@ -436,13 +458,13 @@ __device__ __forceinline__ void run_issuer(const Args& a, uint32_t base, Control
     constexpr uint32_t kFormat = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t kDesc = mma_desc(kFormat, false, !C::kGate, kTileRows, C::kCols);
     constexpr uint32_t kDescDw = mma_desc(kFormat, true, true, kTileRows, C::kCols);
-    const uint32_t items = items_of<T>(a), tmem = c.tmem;
+    const uint32_t tmem = c.tmem;
     const uint32_t full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
     Ring<C::kStages> ring;
     uint32_t n = 0;
     bool fine = true;
-    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
-        const Item it = item_of<T>(a, index);
+    for (Walk walk = walk_of<T>(a); fine && walk.more(); walk.next()) {
+        const Item it = item_of<T>(a, walk.index);
         const bool a_rows = !C::kGate && it.dw;
         const uint32_t desc = a_rows ? kDescDw : kDesc;
         const uint64_t like_a = a_rows ? operand_desc(0, 8192, 1024) : operand_desc(0, 16, 1024);
@@ -479,14 +501,14 @@ template <typename C, typename T, int ACT, typename Args>
 __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Control& c, const LaunchCtl& ctl) {
     const uint32_t warp = (threadIdx.x >> 5) - 4, quarter = warp & 3u, group = warp >> 2, rank = cluster_rank(), lane = lane_id();
     uint8_t* turn = turns + warp * C::kTurnBlocks * kTurnBytes<T>;
-    const uint32_t items = items_of<T>(a), free0 = in_cta(shared_address(&c.free_[0]), 0);
+    const uint32_t free0 = in_cta(shared_address(&c.free_[0]), 0);
     const FfnProblem& p = a.p;
     const uint32_t tmem = c.tmem + (quarter * 32u << 16), sums = tmem + 2 * C::kCols;
     constexpr uint32_t kBlocks = C::kGate ? C::kCols / 64 : C::kCols / 32;
     uint32_t n = 0;
     bool fine = true;
-    for (uint32_t index = blockIdx.x >> 1; fine && index < items; index += gridDim.x >> 1) {
-        const Item it = item_of<T>(a, index);
+    for (Walk walk = walk_of<T>(a); fine && walk.more(); walk.next()) {
+        const Item it = item_of<T>(a, walk.index);
         const uint32_t row = it.row * kTileRows + rank * 128 + quarter * 32;      // the warp's first
         // dh of the warp's blocks, while the accumulator is still collected
         constexpr uint32_t kOwn = C::kGate ? kBlocks / C::kGroups : 1;
@@ -770,6 +792,8 @@ inline uint8_t* regions_of(const FfnProblem& p) {
 
 // Columns of a products tile: the running sums of 4-byte elements take the other half of tensor memory.
 constexpr uint32_t product_cols(uint64_t size) { return size == 4 ? 128 : 256; }
+// Shares the items of a products kernel out to `pairs` pairs of CTAs.
+void balance(ProductsArgs* a, uint32_t pairs);
 // Hidden columns of a gate tile of 2-byte elements, times two.
 uint32_t gate_cols(uint32_t tile_rows, uint32_t f);
 
@@ -872,6 +896,7 @@ cudaError_t launch_all(const FfnProblem& p, bool backward, const LaunchCtl& ctl,
         !make_operand_map(&maps[3], wu, p.dtype, kStep))
         return cudaErrorInvalidValue;
     const uint64_t items = static_cast<uint64_t>(items_of(a.dx)) + items_of(a.dw);
+    balance(&a, items < kPairs ? static_cast<uint32_t>(items) : kPairs);
     e = launch_kernel<Config<false, false, product_cols(sizeof(T)), 8, T>, T, 0>(maps, a, items, ctl, stream);
     if (e == cudaSuccess && p.dx != nullptr && a.dx.splits > 1) e = join<T>(a.dx, p.dx, nullptr, p.ld_dx, p.m, p.k, stream);
     if (e == cudaSuccess && p.dwg != nullptr && a.dw.splits > 1) e = join<T>(a.dw, p.dwg, p.dwu, p.ld_dw, p.f, p.k, stream);
