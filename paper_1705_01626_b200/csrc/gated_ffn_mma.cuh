@@ -1,6 +1,6 @@
 // The gated feed-forward block on the matrix units (tcgen05).
 //
-//   gate kernel      G and U of 256 rows and up to 128 hidden columns: A = x, B = the tile's rows of Wg next to those
+//   gate kernel      G and U of 256 rows and 64, 96 or 128 hidden columns: A = x, B = the tile's rows of Wg next to those
 //                    of Wu, so that an accumulator holds G and U of the same elements and its reader has both at hand.
 //                    The reader writes h (forward), or dG and dU (backward, after reading dh).
 //   products kernel  256 x 256 tiles of dx (A = dG then dU, B = Wg then Wu, one reduction over both) and of dWg and
@@ -9,7 +9,7 @@
 // A pair of CTAs on two SMs shares one tile (cta_group::2): each holds half of A's and half of B's rows, and the
 // accumulator of its half of the output rows.  In the gate kernel one CTA brings Wg's rows and the other Wu's.
 // Operands arrive by TMA in 128-byte swizzled steps of 64 reduction elements through a ring; one thread issues the
-// matrix instructions; eight or sixteen warps read the finished accumulator while the other of two collects the next
+// matrix instructions; eight to sixteen warps read the finished accumulator while the other of two collects the next
 // tile.  Operands whose rows, not their reduction, are contiguous in memory (B of dx, both of dW) are taken as they lie,
 // by the descriptors' major bits: nothing is transposed.
 //
@@ -18,9 +18,9 @@
 //
 // 4-byte elements: each operand is split into three bf16 planes (x = high + middle + low, 8 bits each: all 24), and
 // the six products of planes that reach 2^-24 of the whole are six parts of one long reduction, the small ones first.
-// On the ordinary units the same sums took four times as long (1000 x 1024 x 2752: 324 us against 84).
+// On the ordinary units the same sums took five times as long (1000 x 1024 x 2752: 324 us against 65).
 //
-// Bound by the matrix unit: a step of a 256-column tile takes 515 cycles of the 512 that its instructions need.  8192 x
+// Bound by the matrix unit, whose instructions follow each other without a pause in tiles of 256 columns.  8192 x
 // 4096 x 10944 bf16: forward 881 us from a cool start (1.67 PFLOP/s), 1.0 ms under the power limit (1.45 PFLOP/s),
 // backward 3.2 ms (1.36 PFLOP/s).  Tiles of few steps are bound by their readers and by filling the ring.
 #pragma once
@@ -205,13 +205,24 @@ __device__ __forceinline__ void move_block(uint8_t* turn, T* at, uint64_t ld, in
             if (STORE) { if (r < rows) *there = *here; }
             else *here = r < rows ? *there : make_uint4(0, 0, 0, 0);
         }
-    } else {
-#pragma unroll 8
-        for (uint32_t r = 0; r < 32; ++r) {
-            T* here = reinterpret_cast<T*>(turn_at<T>(turn, r, lane / kPer)) + lane % kPer;
-            const bool exists = r < rows && lane < cols;
-            if (STORE) { if (exists) at[r * ld + lane] = *here; }
-            else *here = exists ? at[r * ld + lane] : from_float<T>(0.0f);
+    } else if (lane < cols || !STORE) {
+        // a row at a time; the places of a row's pieces repeat every eight rows
+        constexpr uint32_t kPlaces = sizeof(T) == 4 ? 8 : 4;
+        uint32_t place[kPlaces];
+#pragma unroll
+        for (uint32_t i = 0; i < kPlaces; ++i) place[i] = 16 * ((lane / kPer) ^ i) + lane % kPer * sizeof(T);
+        const uint32_t count = rows < 32 ? static_cast<uint32_t>(rows) : 32;
+        const bool exists = lane < cols;
+        T* there = at + lane;
+#pragma unroll 1
+        for (uint32_t r0 = 0; r0 < 32; r0 += 8) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                T* here = reinterpret_cast<T*>(turn + (r0 + i) * 32 * sizeof(T) + place[sizeof(T) == 4 ? i : i >> 1]);
+                if (STORE) { if (r0 + i < count) *there = *here; }
+                else *here = exists && r0 + i < count ? *there : from_float<T>(0.0f);
+                there += ld;
+            }
         }
     }
     __syncwarp();
