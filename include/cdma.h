@@ -357,7 +357,9 @@ typedef struct {
 
 /* Bytes of device scratch of a forward (backward = 0) or backward (1) call; 0 for a
  * descriptor that the calls refuse.  The backward pass keeps the gradients of G and U
- * there (2 m f elements). */
+ * there (2 m f elements), where its products are cut their sums in 32 bits, and both
+ * passes keep copies of operands whose rows do not start on 16 bytes.  CDMA_F32: 6 bytes
+ * for each element of those gradients and of x, Wg and Wu. */
 uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int backward);
 
 /*
@@ -368,7 +370,8 @@ uint64_t cdma_gated_ffn_workspace_bytes(const cdma_gated_ffn_desc* desc, int bac
  * Backward: from x, Wg, Wu and dh, with e = D dh: dU = e act(G), dG = e U act'(G),
  * dx = dG Wg + dU Wu, dWg = dG^T x, dWu = dU^T x.  G and U are computed again from the
  * inputs: the forward pass leaves nothing to keep.  For 2-byte types dG and dU are
- * rounded to the element type between the two products.  d_dx may be NULL, and d_dwg
+ * rounded to the element type between the two products.  Sums that overflow or meet
+ * infinities may come out as NaN where one order of adding would give an infinity.  d_dx may be NULL, and d_dwg
  * and d_dwu both may, when that gradient is not wanted (not all three).
  *
  * Outputs must not overlap inputs, one another or the workspace, except as disjoint

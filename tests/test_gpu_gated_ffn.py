@@ -368,3 +368,23 @@ def test_signs_of_gates_near_zero(dtype, m):
     sure = (g.abs() > 2.0 ** -21) & (u.abs() > 2.0 ** -10)
     assert sure.double().mean() > 0.99
     assert torch.equal((dg != 0)[sure], (g > 0)[sure])
+
+
+def test_maps_past_thirty_two_bits():
+    # h, dh, dG and dU of more than 2^32 elements: the last rows and the last hidden columns against the formulas
+    m, k, f, dtype = 270_000, 64, 16_000, torch.bfloat16
+    b = Block(m, k, f, dtype, "silu")
+    b.forward()
+    last = slice(m - 64, m)
+    want = gf.forward(b.x[last], b.wg, b.wu, "silu")
+    within(b.hw[last], want, "h")
+    del b.hw
+    b.workspace(1)
+    r = B.cdma_gated_ffn_backward(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.dhw.data_ptr(), b.dxw.data_ptr(),
+                                  b.dwgw.data_ptr(), b.dwuw.data_ptr(), b.ws.data_ptr(), b.ws_bytes, 0)
+    assert r == 2 * (m * k + 2 * f * k), B.status_string(r)
+    within(b.dxw[last], gf.backward(b.x[last], b.wg, b.wu, b.dhw[last], "silu"), "dx")
+    of = slice(f - 32, f)
+    want = gf.backward(b.x, b.wg[of], b.wu[of], b.dhw[:, of], "silu")
+    within(b.dwgw[of], want, "dwg")
+    within(b.dwuw[of], want, "dwu")
