@@ -285,9 +285,9 @@ __device__ __forceinline__ void fetch_dh(uint8_t* turn, uint32_t (&words)[16], c
 }
 
 // 32 hidden columns of the warp's 32 rows: h, or dG and dU; G at tensor-memory place `g`, U at `u`.  dh: in `words`, or
-// in the turning block for 4-byte elements.  Eight columns at
-// a time, two turns unrolled: over all columns the code does not fit the instruction cache, and the first tile
-// of a launch, often its only one, waited for instructions most of the time (GELU: 37,000 cycles for 32 columns).
+// in the turning block for 4-byte elements.  Eight columns at a time, two turns unrolled: over all columns the code does
+// not fit the instruction cache, and the first tile of a launch, often its only one, waited for instructions most of the
+// time (GELU: 37,000 cycles for 32 columns).
 template <typename T, int ACT, bool BACKWARD>
 __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, uint32_t row, uint32_t col, uint32_t g, uint32_t u,
                                             uint32_t (&words)[16]) {
