@@ -410,7 +410,7 @@ __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map
     const uint32_t rank = cluster_rank();
     const uint32_t full = in_cta(shared_address(&c.full[0]), 0), own_full = shared_address(&c.full[0]), empty = shared_address(&c.empty[0]);
     Ring<C::kStages> ring;
-    bool fine = true;
+    bool fine = true, begun = false;
     if (ctl.stall_tile == blockIdx.x >> 1) return;      // test hook: nothing is ever brought
     for (Walk walk = walk_of<T>(a); fine && walk.more(); walk.next()) {
         const Item it = item_of<T>(a, walk.index);
@@ -427,6 +427,8 @@ __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map
             const uint32_t plane_a = sizeof(T) == 4 ? kPlaneOfA >> (4 * product) & 15u : 0;
             const uint32_t plane_b = sizeof(T) == 4 ? kPlaneOfB >> (4 * product) & 15u : 0;
             const uint32_t of_g = ((it.dw ? it.second : up) ? Planes<T>::count : 0) + plane_a;
+            if (!begun) wait_for_previous();
+            begun = true;
             if (elect_one()) {
                 if (rank == 0) mbar_expect(own_full + 8 * ring.stage, 2 * C::kStageBytes);
                 if constexpr (C::kGate) {
@@ -517,10 +519,12 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
     const uint32_t tmem = c.tmem + (quarter * 32u << 16), sums = tmem + 2 * C::kCols;
     constexpr uint32_t kBlocks = C::kGate ? C::kCols / 64 : C::kCols / 32;
     uint32_t n = 0;
-    bool fine = true;
+    bool fine = true, begun = false;
     for (Walk walk = walk_of<T>(a); fine && walk.more(); walk.next()) {
         const Item it = item_of<T>(a, walk.index);
         const uint32_t row = it.row * kTileRows + rank * 128 + quarter * 32;      // the warp's first
+        if (!begun) wait_for_previous();
+        begun = true;
         // dh of the warp's blocks, while the accumulator is still collected
         constexpr uint32_t kOwn = C::kGate ? kBlocks / C::kGroups : 1;
         static_assert(sizeof(T) == 2 || kOwn == 1, "the turning block holds one block of dh");
@@ -687,9 +691,12 @@ ffn_mma_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     cluster_sync();
     tcgen05_fence_after();
     let_next_start();
-    wait_for_previous();
-    if (C::kGate && blockIdx.x == 0 && threadIdx.x == 96) init_decode_result(a.p.ws, ctl, a.p.result_bytes);
-
+    if (C::kGate && blockIdx.x == 0 && threadIdx.x == 96) {
+        wait_for_previous();
+        init_decode_result(a.p.ws, ctl, a.p.result_bytes);
+    }
+    // Each role waits for the kernel in front where it first touches memory: by then it has found its first item, which
+    // takes 1200 to 2700 cycles while its instructions and arguments come in.
     if (warp == 0) run_loader<C, T>(a, &map_x, &map_g, &map_wg, &map_wu, base, c, ctl);
     else if (warp == 1 && cluster_rank() == 0) run_issuer<C, T>(a, base, c, ctl);
     else if (warp >= 4) run_readers<C, T, ACT>(a, turns, c, ctl);

@@ -84,8 +84,10 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
     __syncthreads();
     tcgen05_fence_after();
     let_next_start();
-    wait_for_previous();
-    if (blockIdx.x == 0 && threadIdx.x == 128) init_decode_result(p.ws, ctl, p.result_bytes);
+    if (blockIdx.x == 0 && threadIdx.x == 128) {
+        wait_for_previous();
+        init_decode_result(p.ws, ctl, p.result_bytes);
+    }
 
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -93,6 +95,7 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             if (ctl.stall_tile == blockIdx.x) break;      // test hook: nothing is ever brought
             if (!mbar_wait(shared_address(&c.empty[stage]), phase ^ 1u, &c.gave_up, ctl.wait_limit_ns)) break;
             const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
+            if (s == first) wait_for_previous();
             if (elect_one()) {
                 mbar_expect(bar, stage_bytes);
 #pragma unroll
@@ -134,6 +137,7 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
         if (fine && elect_one()) mma_commit_single(shared_address(&c.done));
     }
     __syncwarp();
+    wait_for_previous();      // before h is written or dh read
     const bool fine = mbar_wait(shared_address(&c.done), 0, &c.gave_up, ctl.wait_limit_ns);
     tcgen05_fence_after();
     __syncwarp();
