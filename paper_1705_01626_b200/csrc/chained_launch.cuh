@@ -12,6 +12,12 @@
 namespace cdma {
 
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The same in front of bulk copies: they read memory by another way than the stores of the kernel in front went, and the
+// fence orders the two.
+__device__ __forceinline__ void wait_before_copies() {
+    wait_for_previous();
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+}
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // cluster: CTAs per cluster, 0 where the kernel has that fixed or has none.

@@ -317,7 +317,8 @@ __device__ __forceinline__ void finish_gate(const GateArgs& a, uint8_t* turn, ui
             for (int i = 0; i < 12; ++i) words[i] = words[i + 4];
         }
         uint32_t gw[8], uw[8];
-        tmem_load_wait();
+        tmem_landed(next_g);
+        tmem_landed(next_u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) { gw[j] = next_g[j]; uw[j] = next_u[j]; }
         if (c + 8 < 32) {
@@ -427,7 +428,7 @@ __device__ __forceinline__ void run_loader(const Args& a, const CUtensorMap* map
             const uint32_t plane_a = sizeof(T) == 4 ? kPlaneOfA >> (4 * product) & 15u : 0;
             const uint32_t plane_b = sizeof(T) == 4 ? kPlaneOfB >> (4 * product) & 15u : 0;
             const uint32_t of_g = ((it.dw ? it.second : up) ? Planes<T>::count : 0) + plane_a;
-            if (!begun) wait_for_previous();
+            if (!begun) wait_before_copies();
             begun = true;
             if (elect_one()) {
                 if (rank == 0) mbar_expect(own_full + 8 * ring.stage, 2 * C::kStageBytes);
@@ -556,7 +557,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
 #pragma unroll
                 for (uint32_t side = 0; side < 2; ++side) {
                     tmem_load32(at + side * kUp, v);
-                    tmem_load_wait();
+                    tmem_landed(v);
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[side][j] = s != it.first ? sum[side][j] + __uint_as_float(v[j]) : __uint_as_float(v[j]);
                 }
@@ -576,12 +577,18 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
 #pragma unroll 1
                 for (uint32_t i = group; i < C::kCols / 32; i += C::kGroups) {
                     const uint32_t at = i * 32;
-                    uint32_t v[32], w[32];
+                    uint32_t v[32];
                     tmem_load32(from + at, v);
-                    if (s != it.first) tmem_load32(sums + at, w);
-                    tmem_load_wait();
+                    if (s != it.first) {
+                        uint32_t w[32];
+                        tmem_load32(sums + at, w);
+                        tmem_landed(v);
+                        tmem_landed(w);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = s != it.first ? __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(w[j])) : v[j];
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(w[j]));
+                    } else {
+                        tmem_landed(v);
+                    }
                     tmem_store32(sums + at, v);
                 }
                 tmem_store_wait();
@@ -609,7 +616,7 @@ __device__ __forceinline__ void run_readers(const Args& a, uint8_t* turns, Contr
             for (uint32_t i = group; i < kBlocks; i += C::kGroups) {
                 const uint32_t col = it.col * C::kCols + i * 32;
                 uint32_t v[32];
-                tmem_load_wait();
+                tmem_landed(next);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] = next[j];
                 if (i + C::kGroups < kBlocks) tmem_load32(from + (i + C::kGroups) * 32, next);

@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
             if (ctl.stall_tile == blockIdx.x) break;      // test hook: nothing is ever brought
             if (!mbar_wait(shared_address(&c.empty[stage]), phase ^ 1u, &c.gave_up, ctl.wait_limit_ns)) break;
             const uint32_t bar = shared_address(&c.full[stage]), dst = base + stage * stage_bytes;
-            if (s == first) wait_for_previous();
+            if (s == first) wait_before_copies();
             if (elect_one()) {
                 mbar_expect(bar, stage_bytes);
 #pragma unroll
@@ -147,12 +147,12 @@ __global__ void __launch_bounds__(kThreads) ffn_stream_kernel(const __grid_const
         for (uint32_t col = 16 * (warp >> 2); col < a.cols; col += 32) {
             uint32_t v[16];
             tmem_load16(c.tmem + ((warp & 3u) * 32u << 16) + col, v);
-            tmem_load_wait();
+            tmem_landed(v);
             if constexpr (sizeof(T) == 4) {
                 for (uint32_t other = 1; other < min(a.accumulators, last - first + 1); ++other) {
                     uint32_t w[16];
                     tmem_load16(c.tmem + ((warp & 3u) * 32u << 16) + other * a.cols + col, w);
-                    tmem_load_wait();
+                    tmem_landed(w);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
                 }

@@ -169,6 +169,15 @@ __device__ __forceinline__ void tmem_store32(uint32_t tmem, const uint32_t (&v)[
                    "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(tmem) : "memory");
 }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads under way.  Their registers pass through a statement behind the wait: nothing else would keep the
+// compiler from using them in front of it, where they hold what was there before whenever the load takes longer than usual.
+template <int N>
+__device__ __forceinline__ void tmem_landed(uint32_t (&v)[N]) {
+    static_assert(N % 8 == 0, "");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]) :: "memory");
+}
 
 }  // namespace cdma

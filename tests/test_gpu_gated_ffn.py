@@ -232,6 +232,28 @@ def test_inputs_written_right_before_the_call(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,f", [(40, 512, 640), (130, 257, 391), (513, 320, 640)])
+def test_nothing_is_read_before_it_is_written(m, k, f, dtype):
+    # the workspace holds NaNs in front of every call: a gradient that one kernel reads before another wrote it would show
+    b = Block(m, k, f, dtype, "relu", 0.25)
+    want = {n: t.clone() for n, t in b.backward().items()}
+    stream = torch.cuda.current_stream().cuda_stream
+    words = torch.zeros(2, dtype=torch.int64).pin_memory()
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    flush = torch.empty(1 << 27, dtype=torch.uint8, device="cuda")
+    for i in range(400):
+        if i % 4 == 0:
+            flush.fill_(i & 127)
+        b.ws[:b.ws_bytes].fill_(0x7f if dtype == torch.float16 else 0xff)
+        assert B.cdma_gated_ffn_backward_async(b.desc, b.x.data_ptr(), b.wg.data_ptr(), b.wu.data_ptr(), b.dh.data_ptr(),
+                                               b.dxw.data_ptr(), b.dwgw.data_ptr(), b.dwuw.data_ptr(), b.ws.data_ptr(),
+                                               b.ws_bytes, stream, words.data_ptr()) == B.OK
+        for n, t in (("dx", b.dxw), ("dwg", b.dwgw), ("dwu", b.dwuw)):
+            wrong += (t[:, :k] != want[n]).sum()
+    assert int(wrong) == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_sizes_of_zero(dtype):
     for m, k, f in ((0, 8, 16), (4, 0, 16), (4, 8, 0), (0, 0, 0)):
         b = Block(m, k, f, dtype)
